@@ -304,6 +304,82 @@ ADAPTION_API int adaption_maxpool2x2(adaption_qtensor x, int32_t N, int32_t H, i
 ADAPTION_API int adaption_choose_frac_bits_from_acc(int64_t max_abs_acc, int32_t acc_frac_bits,
                                        int32_t n_bits, adaption_qfmt* h_out);
 
+/* ---- microscaled 4-bit floating point ----------------------------------------------------------
+ * Beside the one decimal point per tensor of the formats above: tensors whose rows are cut into blocks
+ * of `block` = 32 or 16 consecutive elements, each block with a scale of its own.  An element is a code c
+ * of 4 bits (E2M1: bit 3 the sign, bits 0-2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6) and stands for c * step:
+ *   block 32: step = 2^(b - 127), b the block's scale byte (E8M0; 255 is NaN and never written);
+ *             `exp` has to be 0;
+ *   block 16: step = e4m3(b) * 2^exp, b a byte of E4M3 without sign (at most 448) and exp one
+ *             exponent for the whole tensor, -64 <= exp <= 63 (adaption_fp4_choose_exp).
+ * Storage of a tensor of `outer` rows of `inner` elements:
+ *   codes    rows of c_stride / 2 bytes, two elements a byte, the even one in bits 0-3; c_stride >= inner is
+ *            a multiple of 32.  Behind the last element a row holds zeros.
+ *   scales   adaption_fp4_scale_bytes(outer, inner, block) bytes: tiles of 128 rows x 4 blocks, 512 bytes each, the
+ *            tiles of the same rows one after the other; inside a tile the byte of row r and block j is at
+ *            (r % 32) * 16 + (r / 32) * 4 + j (the order in which the tensor cores take them).  The bytes of blocks
+ *            behind a row's last one are 0; those of rows behind the last row are never read into a result. */
+typedef struct adaption_fp4tensor {
+  void* codes;
+  void* scales;
+  int64_t c_stride;
+  int32_t block;     /* 16 or 32 */
+  int32_t exp;
+} adaption_fp4tensor;
+
+/* Real-valued matrices: rows of elements of one type, `stride` elements apart (at least a row's length).  The
+ * address is aligned to the element; rows whose address and stride are multiples of 16 bytes are read and written
+ * fastest. */
+enum { ADAPTION_F32 = 0, ADAPTION_F16 = 1, ADAPTION_BF16 = 2 };
+typedef struct adaption_matrix {
+  void* data;
+  int64_t stride;
+  int32_t dtype;
+  int32_t reserved;
+} adaption_matrix;
+
+/* Bytes of the scale plane (0 for sizes below 1 or another block length). */
+ADAPTION_API size_t adaption_fp4_scale_bytes(int64_t outer, int64_t inner, int32_t block);
+
+/* Host helper, the counterpart of the decimal point for blocks of 16: the smallest exponent in [-64, 63] with which
+ * the scale of a block that holds max_abs fits E4M3 (max_abs <= 6 * 448 * 2^exp); -64 for 0.  max_abs must
+ * not be negative or NaN. */
+ADAPTION_API int adaption_fp4_choose_exp(float max_abs, int32_t* h_exp);
+
+/* The quantizer (LPAct when relu != 0) into the format of `out`.  Exactly one of x.data (real values) and h_x_q (host
+ * pointer to the descriptor of a fixed-point tensor) is given.  With amax = max |x| over a block:
+ *   block 32: b = clamp(floor(log2 amax) - 2, -127, 127) + 127 (0 for amax = 0);
+ *   block 16: b = E4M3 nearest to amax * 2^-exp / 6, ties to even, at most 448;
+ * and each code is the E2M1 number nearest to x / step, ties to even, at most 6 in magnitude, with the sign of x
+ * (codes are 0 where the step is).  NaN counts as 0, +-Inf as the largest finite float.  The result is fixed bit for bit.
+ * d_stats (may be NULL) accumulates, over the outer*inner elements, codes of value 0 and elements of at least
+ * 7 steps (rounded to the next number beyond 6 and clipped). */
+ADAPTION_API int adaption_fp4_quantize(adaption_matrix x, const adaption_qtensor* h_x_q, size_t outer, size_t inner,
+                                       int32_t relu, adaption_fp4tensor out, adaption_stats* d_stats, void* stream);
+
+/* The values that the codes stand for, rounded once to the type of y (to nearest, ties to even; beyond the type's
+ * range to infinity).  Columns of y behind `inner` stay as they are. */
+ADAPTION_API int adaption_fp4_dequantize(adaption_fp4tensor x, size_t outer, size_t inner, adaption_matrix y,
+                                         void* stream);
+
+/* Inner product of 4-bit operands: y[b,o] = act(sum_k x[b,k] * w[o,k] + bias[o]), x [B][K] and w [O][K] of the same
+ * block length, bias fp32 [O] or NULL, act ReLU if relu != 0, y [B][O].  Products are exact, sums are held in 32-bit
+ * floating point in an order fixed by the sizes (so that the same call gives the same bits), and the result is
+ * rounded once to the type of y.  Rows of y are aligned to the element only.  d_stats (not NULL) counts outputs equal to 0
+ * and takes the status. */
+ADAPTION_API int adaption_fp4_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_fp4tensor x, adaption_fp4tensor w,
+                                     const float* d_bias, int32_t relu, adaption_matrix y, adaption_stats* d_stats,
+                                     void* stream);
+
+/* The same on real activations, which are quantized on the way as adaption_fp4_quantize does with w's block length
+ * and the exponent x_exp.  The workspace takes their codes and scales (its contents need no initialisation); calls that may overlap
+ * on the GPU need one each. */
+ADAPTION_API size_t adaption_fp4_act_ip_workspace_bytes(int64_t B, int64_t K, int64_t O, int32_t block);
+ADAPTION_API int adaption_fp4_act_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_matrix x, int32_t x_exp,
+                                         adaption_fp4tensor w, const float* d_bias, int32_t relu, adaption_matrix y,
+                                         adaption_stats* d_stats, void* d_workspace, size_t workspace_bytes,
+                                         void* stream);
+
 /* Measurement aid for the roofline of the layer calls (no counterpart in the paper): every SM
  * (pair != 0: every pair of SMs working on 256-row tiles) issues 4*iters back-to-back int8
  * tensor-core instructions of shape 128 (256) x bn x 32 on operands resident in shared memory.

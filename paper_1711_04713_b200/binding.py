@@ -50,6 +50,15 @@ class adaption_conv_shape(C.Structure):
                                           "stride_h", "stride_w")]
 
 
+class adaption_fp4tensor(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("c_stride", C.c_int64), ("block", C.c_int32),
+                ("exp", C.c_int32)]
+
+
+class adaption_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
 STATS_BYTES = C.sizeof(adaption_stats)
 EXPORTS = [
     "adaption_measure_range", "adaption_quantize", "adaption_lp_act",
@@ -61,6 +70,8 @@ EXPORTS = [
     "adaption_lp_act_stochastic", "adaption_lp_conv_pool_workspace_bytes", "adaption_lp_conv_pool_fwd",
     "adaption_quantize_batch", "adaption_quantize_batch_stochastic", "adaption_debug_set", "adaption_lp_conv_fwd_stochastic",
     "adaption_lp_ip_fwd_stochastic", "adaption_launches", "adaption_debug_get",
+    "adaption_fp4_scale_bytes", "adaption_fp4_choose_exp", "adaption_fp4_quantize", "adaption_fp4_dequantize",
+    "adaption_fp4_ip_fwd", "adaption_fp4_act_ip_workspace_bytes", "adaption_fp4_act_ip_fwd",
 ]
 HIST_BINS = 17
 
@@ -124,13 +135,24 @@ def load(path: str | None = None):
                                                         C.POINTER(adaption_qfmt)]
     lib.adaption_choose_frac_bits_from_widths.argtypes = [C.POINTER(C.c_uint64), I32, I32, C.c_double,
                                                           C.POINTER(adaption_qfmt)]
+    F4, MAT = adaption_fp4tensor, adaption_matrix
+    lib.adaption_fp4_scale_bytes.argtypes = [I64, I64, I32]
+    lib.adaption_fp4_scale_bytes.restype = SZ
+    lib.adaption_fp4_choose_exp.argtypes = [C.c_float, C.POINTER(I32)]
+    lib.adaption_fp4_quantize.argtypes = [MAT, C.POINTER(adaption_qtensor), SZ, SZ, I32, F4, P, P]
+    lib.adaption_fp4_dequantize.argtypes = [F4, SZ, SZ, MAT, P]
+    lib.adaption_fp4_ip_fwd.argtypes = [I64, I64, I64, F4, F4, P, I32, MAT, P, P]
+    lib.adaption_fp4_act_ip_workspace_bytes.argtypes = [I64, I64, I64, I32]
+    lib.adaption_fp4_act_ip_workspace_bytes.restype = SZ
+    lib.adaption_fp4_act_ip_fwd.argtypes = [I64, I64, I64, MAT, I32, F4, P, I32, MAT, P, P, SZ, P]
     lib.adaption_debug_set.argtypes = [C.c_char_p, C.c_int32]
     lib.adaption_debug_get.argtypes = [C.c_char_p, C.POINTER(C.c_int32)]
     lib.adaption_status_string.argtypes = [C.c_int]
     lib.adaption_status_string.restype = C.c_char_p
     for name in EXPORTS:
         if name not in ("adaption_lp_conv_workspace_bytes", "adaption_lp_ip_workspace_bytes",
-                        "adaption_lp_conv_pool_workspace_bytes", "adaption_status_string"):
+                        "adaption_lp_conv_pool_workspace_bytes", "adaption_status_string",
+                        "adaption_fp4_scale_bytes", "adaption_fp4_act_ip_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     lib.adaption_launches.argtypes = []
     lib.adaption_launches.restype = C.c_uint64
@@ -140,7 +162,7 @@ def load(path: str | None = None):
     spec = importlib.util.spec_from_file_location("_adaption_native", _build.NATIVE_PATH)
     native = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(native)
-    native.bind(os.path.abspath(path), AdaptionError, *_stream_getters())
+    native.bind(os.path.abspath(path), AdaptionError, *_stream_getters(), torch.float32, torch.float16, torch.bfloat16)
     _native = native
     _lib = lib
     return lib
@@ -250,6 +272,39 @@ class QTensor:
         cs = inner if c_stride is None else c_stride
         assert outer * cs == self.outer * self.c_stride
         return QTensor(outer, inner, cs, self.n_bits, self.frac_bits, self.lo, self.hi, self.q16)
+
+
+@dataclass
+class Fp4Tensor:
+    """A microscaled 4-bit tensor on the device: logical shape (outer, inner), row pitch ``c_stride`` elements (a
+    multiple of 32).  ``codes`` (outer * c_stride / 2 bytes) and ``scales`` (adaption_fp4_scale_bytes) are
+    contiguous uint8 tensors; ``block`` is 16 or 32, ``exp`` the exponent of a tensor with blocks of 16."""
+    outer: int
+    inner: int
+    c_stride: int
+    block: int
+    exp: int
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    def __post_init__(self):
+        if self.block not in (16, 32) or self.c_stride % 32 or self.c_stride < self.inner or self.outer < 0 or self.inner < 1:
+            raise AdaptionError(ERR_INVALID_ARG, "Fp4Tensor")
+        for t, need in ((self.codes, self.outer * (self.c_stride // 2)),
+                        (self.scales, fp4_scale_bytes(self.outer, self.inner, self.block))):
+            if t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() < need or t.device != self.codes.device:
+                raise AdaptionError(ERR_INVALID_ARG, "Fp4Tensor")
+
+    @staticmethod
+    def empty(outer: int, inner: int, block: int = 16, exp: int = 0, c_stride: int | None = None,
+              device="cuda") -> "Fp4Tensor":
+        cs = pad_to(inner, 32) if c_stride is None else c_stride
+        codes = torch.empty(max(0, outer * (cs // 2)), dtype=torch.uint8, device=device)
+        scales = torch.empty(fp4_scale_bytes(outer, inner, block), dtype=torch.uint8, device=device)
+        return Fp4Tensor(outer, inner, cs, block, exp, codes, scales)
+
+    def c_struct(self) -> adaption_fp4tensor:
+        return adaption_fp4tensor(_ptr(self.codes), _ptr(self.scales), self.c_stride, self.block, self.exp)
 
 
 def new_stats(device="cuda") -> torch.Tensor:
@@ -436,3 +491,45 @@ def adaption_choose_frac_bits_from_acc(max_abs_acc: int, acc_frac_bits: int, n_b
     _check(load().adaption_choose_frac_bits_from_acc(max_abs_acc, acc_frac_bits, n_bits, C.byref(out)),
            "adaption_choose_frac_bits_from_acc")
     return int(out.frac_bits)
+
+
+# --------------------------------------------------------------------------- microscaled 4-bit floating point
+# Real-valued tensors (x, y) are 2-D CUDA tensors of float32, float16 or bfloat16 whose rows are contiguous
+# (any pitch of at least a row); tensors lie on the current device.
+def fp4_scale_bytes(outer: int, inner: int, block: int) -> int:
+    """adaption_fp4_scale_bytes: bytes of the scale plane."""
+    return -(-outer // 128) * -(--(-inner // block) // 4) * 512 if outer > 0 and inner > 0 else 0
+
+
+def adaption_fp4_choose_exp(max_abs: float) -> int:
+    out = C.c_int32()
+    _check(load().adaption_fp4_choose_exp(float(max_abs), C.byref(out)), "adaption_fp4_choose_exp")
+    return int(out.value)
+
+
+def adaption_fp4_quantize(x: "torch.Tensor | QTensor", outer: int, inner: int, out: Fp4Tensor, relu: bool = False,
+                          d_stats: torch.Tensor | None = None):
+    """x: a real-valued (outer, inner) tensor, or a stored fixed-point one."""
+    _calls().fp4_quantize(x, outer, inner, out, relu, d_stats)
+
+
+def adaption_fp4_dequantize(x: Fp4Tensor, outer: int, inner: int, y: torch.Tensor):
+    _calls().fp4_dequantize(x, outer, inner, y)
+
+
+def adaption_fp4_ip_fwd(B: int, K: int, O: int, x: Fp4Tensor, w: Fp4Tensor, bias: torch.Tensor | None, relu: bool,
+                        y: torch.Tensor, d_stats: torch.Tensor):
+    """bias: float32 [O] or None; y: a real-valued (B, O) tensor."""
+    _calls().fp4_ip_fwd(B, K, O, x, w, bias, relu, y, d_stats)
+
+
+def fp4_act_ip_workspace_bytes(B: int, K: int, O: int, block: int) -> int:
+    """adaption_fp4_act_ip_workspace_bytes."""
+    return int(load().adaption_fp4_act_ip_workspace_bytes(B, K, O, block))
+
+
+def adaption_fp4_act_ip_fwd(B: int, K: int, O: int, x: torch.Tensor, x_exp: int, w: Fp4Tensor,
+                            bias: torch.Tensor | None, relu: bool, y: torch.Tensor, d_stats: torch.Tensor,
+                            workspace: torch.Tensor | None):
+    """x: a real-valued (B, K) tensor, quantized on the way with w's block length and the exponent x_exp."""
+    _calls().fp4_act_ip_fwd(B, K, O, x, x_exp, w, bias, relu, y, d_stats, workspace)

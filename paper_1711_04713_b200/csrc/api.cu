@@ -3,7 +3,10 @@
 #include <cstdlib>
 #include <cstring>
 
+#include <cmath>
+
 #include "common.cuh"
+#include "fp4.cuh"
 
 namespace adaption {
 int cuda_failure(cudaError_t e, const char* where) {
@@ -217,6 +220,32 @@ static ConvPoolPlan plan_conv_pool(GemmProblem g, int32_t algo) {
   pl.total = pl.conv_ws + (size_t)planes * pl.plane;
   return pl;
 }
+
+// ---- inner product of 4-bit operands ---------------------------------------------------------
+// Arguments that both calls take; x is checked by the caller.
+static int build_fp4_problem(int64_t B, int64_t K, int64_t O, const adaption_fp4tensor& w, const float* bias, int32_t relu,
+                             const adaption_matrix& y, adaption_stats* stats, void* stream, Fp4Problem& g) {
+  if (B < 0 || K <= 0 || O <= 0) return ADAPTION_ERR_INVALID_ARG;
+  if (K > kFp4MaxInner) return ADAPTION_ERR_K_TOO_LARGE;
+  if (B > ((int64_t)1 << 30) || O > ((int64_t)1 << 30)) return ADAPTION_ERR_UNSUPPORTED;
+  int rc = check_fp4(w, K);
+  if (rc != ADAPTION_OK) return rc;
+  if (stats == nullptr) return ADAPTION_ERR_INVALID_ARG;
+  rc = B > 0 ? check_matrix(y, O) : ADAPTION_OK;        // (no rows: nothing of x or y is looked at)
+  if (rc != ADAPTION_OK) return rc;
+  if (bias != nullptr && (reinterpret_cast<uintptr_t>(bias) & 3u) != 0) return ADAPTION_ERR_ALIGNMENT;
+  g.B = B; g.K = K; g.O = O;
+  g.w = w;
+  g.bias = bias;
+  g.relu = relu ? 1 : 0;
+  g.y = y;
+  g.stats = stats;
+  g.stream = reinterpret_cast<cudaStream_t>(stream);
+  return ADAPTION_OK;
+}
+
+// The workspace of the product on real activations: their codes, then their scales.
+static size_t fp4_codes_bytes(int64_t B, int64_t K) { return ((size_t)B * (size_t)((K + 31) / 32 * 16) + 255) & ~(size_t)255; }
 
 }  // namespace adaption
 
@@ -454,6 +483,66 @@ int adaption_choose_frac_bits_from_acc(int64_t max_abs_acc, int32_t acc_frac_bit
   h_out->n_bits = n_bits;
   h_out->frac_bits = n_bits - 1 - m;
   return ADAPTION_OK;
+}
+
+size_t adaption_fp4_scale_bytes(int64_t outer, int64_t inner, int32_t block) {
+  if (outer <= 0 || inner <= 0 || (block != 16 && block != 32)) return 0;
+  return (size_t)((outer + kFp4TileRows - 1) / kFp4TileRows) * (size_t)fp4_groups(inner, block) * kFp4TileBytes;
+}
+
+int adaption_fp4_choose_exp(float max_abs, int32_t* h_exp) {
+  if (h_exp == nullptr || !(max_abs >= 0.f)) return ADAPTION_ERR_INVALID_ARG;
+  int e = -64;
+  while (e < 63 && (double)max_abs > std::ldexp(2688.0, e)) ++e;
+  *h_exp = e;
+  return ADAPTION_OK;
+}
+
+int adaption_fp4_quantize(adaption_matrix x, const adaption_qtensor* h_x_q, size_t outer, size_t inner, int32_t relu,
+                          adaption_fp4tensor out, adaption_stats* d_stats, void* stream) {
+  return fp4_quantize_impl(x, h_x_q, outer, inner, relu, out, d_stats, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int adaption_fp4_dequantize(adaption_fp4tensor x, size_t outer, size_t inner, adaption_matrix y, void* stream) {
+  return fp4_dequantize_impl(x, outer, inner, y, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int adaption_fp4_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_fp4tensor x, adaption_fp4tensor w, const float* d_bias,
+                        int32_t relu, adaption_matrix y, adaption_stats* d_stats, void* stream) {
+  Fp4Problem g;
+  int rc = build_fp4_problem(B, K, O, w, d_bias, relu, y, d_stats, stream, g);
+  if (rc != ADAPTION_OK || B == 0) return rc;
+  rc = check_fp4(x, K);
+  if (rc != ADAPTION_OK) return rc;
+  if (x.block != w.block) return ADAPTION_ERR_INVALID_ARG;
+  g.x = x;
+  return fp4_ip_impl(g);
+}
+
+size_t adaption_fp4_act_ip_workspace_bytes(int64_t B, int64_t K, int64_t O, int32_t block) {
+  if (B <= 0 || K <= 0 || O <= 0 || K > kFp4MaxInner || (block != 16 && block != 32)) return 0;
+  return fp4_codes_bytes(B, K) + adaption_fp4_scale_bytes(B, K, block);
+}
+
+int adaption_fp4_act_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_matrix x, int32_t x_exp, adaption_fp4tensor w,
+                            const float* d_bias, int32_t relu, adaption_matrix y, adaption_stats* d_stats,
+                            void* d_workspace, size_t workspace_bytes, void* stream) {
+  Fp4Problem g;
+  int rc = build_fp4_problem(B, K, O, w, d_bias, relu, y, d_stats, stream, g);
+  if (rc != ADAPTION_OK || B == 0) return rc;
+  rc = check_matrix(x, K);
+  if (rc != ADAPTION_OK) return rc;
+  if (w.block == 32 ? x_exp != 0 : (x_exp < -64 || x_exp > 63)) return ADAPTION_ERR_INVALID_ARG;
+  if (d_workspace == nullptr || workspace_bytes < adaption_fp4_act_ip_workspace_bytes(B, K, O, w.block))
+    return ADAPTION_ERR_WORKSPACE;
+  if (!aligned16(d_workspace)) return ADAPTION_ERR_ALIGNMENT;
+  g.x.codes = d_workspace;
+  g.x.scales = static_cast<uint8_t*>(d_workspace) + fp4_codes_bytes(B, K);
+  g.x.c_stride = (K + 31) / 32 * 32;
+  g.x.block = w.block;
+  g.x.exp = x_exp;
+  rc = fp4_quantize_impl(x, nullptr, (size_t)B, (size_t)K, 0, g.x, nullptr, g.stream);
+  return rc != ADAPTION_OK ? rc : fp4_ip_impl(g);
 }
 
 int adaption_probe_i8_peak(int32_t bn, int32_t pair, int32_t iters, int32_t commit_every, uint64_t* d_cycles,

@@ -24,7 +24,8 @@ namespace {
   X(adaption_width_histogram) X(adaption_lp_conv_workspace_bytes) X(adaption_lp_conv_fwd)                            \
   X(adaption_lp_conv_fwd_stochastic) X(adaption_lp_conv_pool_workspace_bytes) X(adaption_lp_conv_pool_fwd)           \
   X(adaption_lp_ip_workspace_bytes) X(adaption_lp_ip_fwd) X(adaption_lp_ip_fwd_stochastic)                           \
-  X(adaption_lp_ip_fwd_static_ws) X(adaption_maxpool2x2)
+  X(adaption_lp_ip_fwd_static_ws) X(adaption_maxpool2x2)                                                             \
+  X(adaption_fp4_quantize) X(adaption_fp4_dequantize) X(adaption_fp4_ip_fwd) X(adaption_fp4_act_ip_fwd)
 #define DECLARE(f) decltype(&::f) p_##f = nullptr;
 ADAPTION_FUNCTIONS(DECLARE)
 #undef DECLARE
@@ -32,8 +33,10 @@ ADAPTION_FUNCTIONS(DECLARE)
 PyObject* g_error = nullptr;        // AdaptionError
 PyObject* g_device = nullptr;       // () -> current device ordinal
 PyObject* g_stream = nullptr;       // (device) -> raw handle of the current stream
+PyObject* g_dtypes[3] = {};         // the tensor types ADAPTION_F32, ADAPTION_F16, ADAPTION_BF16
 
-PyObject *s_lo, *s_hi, *s_q16, *s_n_bits, *s_frac_bits, *s_c_stride, *s_outer, *s_inner, *s_data_ptr, *s_numel, *s_itemsize;
+PyObject *s_lo, *s_hi, *s_q16, *s_n_bits, *s_frac_bits, *s_c_stride, *s_outer, *s_inner, *s_data_ptr, *s_numel, *s_itemsize,
+    *s_codes, *s_scales, *s_block, *s_exp, *s_dtype, *s_shape, *s_stride, *s_get_device;
 
 bool attr_i64(PyObject* o, PyObject* name, long long* out) {
   PyObject* v = PyObject_GetAttr(o, name);
@@ -475,9 +478,216 @@ PyObject* maxpool(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   return answer(rc, "adaption_maxpool2x2");
 }
 
-// library path, AdaptionError, current device, stream of device
-PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+// ---- microscaled 4-bit floating point.  These calls take tensors of several types and any pitch, so what the C ABI cannot see
+// is checked here: type, shape, contiguous rows, and that the tensors lie on the current device.
+
+PyObject* refuse(const char* where) { return answer(ADAPTION_ERR_INVALID_ARG, where); }
+
+// the current device and its stream
+bool device_stream(long long* device, void** out) {
+  PyObject* d = PyObject_CallNoArgs(g_device);
+  if (d == nullptr) return false;
+  *device = PyLong_AsLongLong(d);
+  PyObject* s = *device == -1 && PyErr_Occurred() ? nullptr : PyObject_CallOneArg(g_stream, d);
+  Py_DECREF(d);
+  if (s == nullptr) return false;
+  *out = PyLong_AsVoidPtr(s);
+  Py_DECREF(s);
+  return !(*out == nullptr && PyErr_Occurred());
+}
+// whether a tensor (or None) lies on `device`: 1, 0, or -1 with an exception
+int lies_on(PyObject* t, long long device) {
+  if (t == Py_None) return 1;
+  PyObject* d = PyObject_CallMethodNoArgs(t, s_get_device);
+  if (d == nullptr) return -1;
+  const long long v = PyLong_AsLongLong(d);
+  Py_DECREF(d);
+  if (v == -1 && PyErr_Occurred()) return -1;
+  return v == device;
+}
+int attr_lies_on(PyObject* o, PyObject* name, long long device) {
+  PyObject* t = PyObject_GetAttr(o, name);
+  if (t == nullptr) return -1;
+  const int r = lies_on(t, device);
+  Py_DECREF(t);
+  return r;
+}
+// 1: `t` is a tensor of type `dtype`
+int has_dtype(PyObject* t, PyObject* dtype) {
+  PyObject* d = PyObject_GetAttr(t, s_dtype);
+  if (d == nullptr) return -1;
+  Py_DECREF(d);
+  return d == dtype;
+}
+bool pair_of(PyObject* seq, long long* a, long long* b) {        // a tuple of two numbers; *a = -1 if it is none
+  *a = *b = -1;
+  if (!PyTuple_Check(seq) || PyTuple_GET_SIZE(seq) != 2) return true;
+  return i64(PyTuple_GET_ITEM(seq, 0), a) && i64(PyTuple_GET_ITEM(seq, 1), b);
+}
+// 2-D tensor of rows x cols -> descriptor: 1, 0 (refused) or -1 (exception)
+int matrix(PyObject* t, long long rows, long long cols, long long device, adaption_matrix* m) {
+  const int here = lies_on(t, device);
+  if (here <= 0) return here;
+  PyObject* d = PyObject_GetAttr(t, s_dtype);
+  if (d == nullptr) return -1;
+  Py_DECREF(d);                     // (types live as long as torch)
+  m->reserved = 0;
+  for (m->dtype = 0; m->dtype < 3 && g_dtypes[m->dtype] != d; ++m->dtype) {
+  }
+  if (m->dtype == 3) return 0;
+  long long r, c, sr, sc;
+  PyObject* shape = PyObject_GetAttr(t, s_shape);
+  if (shape == nullptr) return -1;
+  bool ok = pair_of(shape, &r, &c);
+  Py_DECREF(shape);
+  if (!ok) return -1;
+  if (r != rows || c != cols) return 0;
+  PyObject* stride = PyObject_CallMethodNoArgs(t, s_stride);
+  if (stride == nullptr) return -1;
+  ok = pair_of(stride, &sr, &sc);
+  Py_DECREF(stride);
+  if (!ok) return -1;
+  if (cols > 1 && sc != 1) return 0;
+  // (the pitch of a single row means nothing)
+  m->stride = rows > 1 ? sr : (sr > cols ? sr : cols);
+  return tensor_ptr(t, &m->data) ? 1 : -1;
+}
+// Fp4Tensor of at least rows x cols
+int fp4tensor(PyObject* o, long long rows, long long cols, long long device, adaption_fp4tensor* f) {
+  long long outer, inner, cs, block, exp;
+  if (!attr_i64(o, s_outer, &outer) || !attr_i64(o, s_inner, &inner) || !attr_i64(o, s_c_stride, &cs) ||
+      !attr_i64(o, s_block, &block) || !attr_i64(o, s_exp, &exp))
+    return -1;
+  // (the scale tiles follow from the row length, so a tensor is used at its own)
+  if (outer < rows || inner != cols) return 0;
+  const int a = attr_lies_on(o, s_codes, device), b = a > 0 ? attr_lies_on(o, s_scales, device) : a;
+  if (b <= 0) return b;
+  f->c_stride = cs;
+  f->block = (int32_t)block;
+  f->exp = exp < -1000 || exp > 1000 ? 1000 : (int32_t)exp;
+  return attr_ptr(o, s_codes, &f->codes) && attr_ptr(o, s_scales, &f->scales) ? 1 : -1;
+}
+// fp32 vector of at least n elements, or None
+int bias_vector(PyObject* t, long long n, long long device, void** out) {
+  *out = nullptr;
+  if (t == Py_None) return 1;
+  const int here = lies_on(t, device);
+  if (here <= 0) return here;
+  const int f32 = has_dtype(t, g_dtypes[0]);
+  if (f32 <= 0) return f32;
+  PyObject* stride = PyObject_CallMethodNoArgs(t, s_stride);
+  if (stride == nullptr) return -1;
+  long long step = 0, count = 0;
+  bool ok = PyTuple_Check(stride) && PyTuple_GET_SIZE(stride) == 1 ? i64(PyTuple_GET_ITEM(stride, 0), &step) : true;
+  Py_DECREF(stride);
+  if (!ok || !numel(t, &count)) return -1;
+  if (count < n || (step != 1 && n > 1)) return 0;
+  return tensor_ptr(t, out) ? 1 : -1;
+}
+// counters (or None) on the device
+int counters(PyObject* t, long long device, void** out) {
+  const int here = lies_on(t, device);
+  if (here <= 0) return here;
+  return tensor_ptr(t, out) ? 1 : -1;
+}
+#define TAKE(expr, where)                     \
+  {                                           \
+    const int taken = (expr);                 \
+    if (taken < 0) return nullptr;            \
+    if (taken == 0) return refuse(where);     \
+  }
+
+// x (tensor or QTensor), outer, inner, out, relu, d_stats
+PyObject* fp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(6)
+  const char* const where = "adaption_fp4_quantize";
+  long long outer, inner, dev;
+  int32_t relu;
+  void *stats, *st;
+  adaption_matrix x{};
+  adaption_qtensor q{};
+  adaption_fp4tensor out;
+  if (!i64(a[1], &outer) || !i64(a[2], &inner) || !truth(a[4], &relu) || !device_stream(&dev, &st)) return nullptr;
+  if (outer < 0 || inner < 0) return refuse(where);
+  const bool fixed = PyObject_HasAttr(a[0], s_n_bits);
+  if (fixed) {
+    long long rows, cols;
+    if (!attr_i64(a[0], s_outer, &rows) || !attr_i64(a[0], s_inner, &cols)) return nullptr;
+    if (rows < outer || cols < inner) return refuse(where);
+    TAKE(attr_lies_on(a[0], s_lo, dev), where)
+    if (!qtensor(a[0], &q)) return nullptr;
+  } else {
+    TAKE(matrix(a[0], outer, inner, dev, &x), where)
+  }
+  TAKE(fp4tensor(a[3], outer, inner, dev, &out), where)
+  TAKE(counters(a[5], dev, &stats), where)
+  CALL(p_adaption_fp4_quantize(x, fixed ? &q : nullptr, (size_t)outer, (size_t)inner, relu, out, (adaption_stats*)stats, st))
+  return answer(rc, where);
+}
+
+// x, outer, inner, y
+PyObject* fp4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   ARGS(4)
+  const char* const where = "adaption_fp4_dequantize";
+  long long outer, inner, dev;
+  void* st;
+  adaption_fp4tensor x;
+  adaption_matrix y;
+  if (!i64(a[1], &outer) || !i64(a[2], &inner) || !device_stream(&dev, &st)) return nullptr;
+  if (outer < 0 || inner < 0) return refuse(where);
+  TAKE(fp4tensor(a[0], outer, inner, dev, &x), where)
+  TAKE(matrix(a[3], outer, inner, dev, &y), where)
+  CALL(p_adaption_fp4_dequantize(x, (size_t)outer, (size_t)inner, y, st))
+  return answer(rc, where);
+}
+
+// B, K, O, x, w, bias, relu, y, d_stats
+PyObject* fp4_ip_fwd(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(9)
+  const char* const where = "adaption_fp4_ip_fwd";
+  long long B, K, O, dev;
+  int32_t relu;
+  void *bias, *stats, *st;
+  adaption_fp4tensor x, w;
+  adaption_matrix y;
+  if (!i64(a[0], &B) || !i64(a[1], &K) || !i64(a[2], &O) || !truth(a[6], &relu) || !device_stream(&dev, &st)) return nullptr;
+  TAKE(fp4tensor(a[3], B, K, dev, &x), where)
+  TAKE(fp4tensor(a[4], O, K, dev, &w), where)
+  TAKE(bias_vector(a[5], O, dev, &bias), where)
+  TAKE(matrix(a[7], B, O, dev, &y), where)
+  TAKE(counters(a[8], dev, &stats), where)
+  CALL(p_adaption_fp4_ip_fwd(B, K, O, x, w, (const float*)bias, relu, y, (adaption_stats*)stats, st))
+  return answer(rc, where);
+}
+
+// B, K, O, x, x_exp, w, bias, relu, y, d_stats, workspace
+PyObject* fp4_act_ip_fwd(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(11)
+  const char* const where = "adaption_fp4_act_ip_fwd";
+  long long B, K, O, dev, x_exp;
+  int32_t relu;
+  size_t wsb;
+  void *bias, *stats, *ws, *st;
+  adaption_fp4tensor w;
+  adaption_matrix x, y;
+  if (!i64(a[0], &B) || !i64(a[1], &K) || !i64(a[2], &O) || !i64(a[4], &x_exp) || !truth(a[7], &relu) ||
+      !device_stream(&dev, &st))
+    return nullptr;
+  if (x_exp < -1000 || x_exp > 1000) return refuse(where);
+  TAKE(matrix(a[3], B, K, dev, &x), where)
+  TAKE(fp4tensor(a[5], O, K, dev, &w), where)
+  TAKE(bias_vector(a[6], O, dev, &bias), where)
+  TAKE(matrix(a[8], B, O, dev, &y), where)
+  TAKE(counters(a[9], dev, &stats), where)
+  TAKE(lies_on(a[10], dev), where)
+  if (!workspace(a[10], &ws, &wsb)) return nullptr;
+  CALL(p_adaption_fp4_act_ip_fwd(B, K, O, x, (int32_t)x_exp, w, (const float*)bias, relu, y, (adaption_stats*)stats, ws, wsb, st))
+  return answer(rc, where);
+}
+
+// library path, AdaptionError, current device, stream of device, the types of ADAPTION_F32, _F16 and _BF16
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(7)
   const char* path = PyUnicode_AsUTF8(a[0]);
   if (path == nullptr) return nullptr;
   void* lib = dlopen(path, RTLD_NOW | RTLD_LOCAL);
@@ -493,7 +703,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   }
   ADAPTION_FUNCTIONS(RESOLVE)
 #undef RESOLVE
-  for (int k = 1; k < 4; ++k) Py_INCREF(a[k]);
+  for (int k = 1; k < 7; ++k) Py_INCREF(a[k]);
+  for (int k = 0; k < 3; ++k) Py_XSETREF(g_dtypes[k], a[4 + k]);
   Py_XSETREF(g_error, a[1]);
   Py_XSETREF(g_device, a[2]);
   Py_XSETREF(g_stream, a[3]);
@@ -506,7 +717,8 @@ PyMethodDef methods[] = {METHOD(bind), METHOD(measure_range), METHOD(quantize), 
                          METHOD(lp_act_stochastic), METHOD(bit_histogram), METHOD(width_histogram), METHOD(conv_workspace),
                          METHOD(conv_pool_workspace), METHOD(ip_workspace), METHOD(conv_fwd), METHOD(conv_fwd_stochastic),
                          METHOD(conv_pool_fwd), METHOD(ip_fwd), METHOD(ip_fwd_stochastic), METHOD(ip_fwd_static_ws),
-                         METHOD(maxpool), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(maxpool), METHOD(fp4_quantize), METHOD(fp4_dequantize), METHOD(fp4_ip_fwd), METHOD(fp4_act_ip_fwd),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_adaption_native", "Argument marshalling of the C ABI.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 
@@ -516,7 +728,8 @@ PyMODINIT_FUNC PyInit__adaption_native() {
   struct { PyObject** o; const char* s; } names[] = {
       {&s_lo, "lo"}, {&s_hi, "hi"}, {&s_q16, "q16"}, {&s_n_bits, "n_bits"}, {&s_frac_bits, "frac_bits"},
       {&s_c_stride, "c_stride"}, {&s_outer, "outer"}, {&s_inner, "inner"}, {&s_data_ptr, "data_ptr"}, {&s_numel, "numel"},
-      {&s_itemsize, "itemsize"}};
+      {&s_itemsize, "itemsize"}, {&s_codes, "codes"}, {&s_scales, "scales"}, {&s_block, "block"}, {&s_exp, "exp"},
+      {&s_dtype, "dtype"}, {&s_shape, "shape"}, {&s_stride, "stride"}, {&s_get_device, "get_device"}};
   for (auto& n : names) {
     *n.o = PyUnicode_InternFromString(n.s);
     if (*n.o == nullptr) return nullptr;
