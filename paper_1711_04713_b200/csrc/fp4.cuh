@@ -17,8 +17,9 @@ inline int64_t fp4_blocks(int64_t inner, int block) { return (inner + block - 1)
 inline int64_t fp4_groups(int64_t inner, int block) { return (fp4_blocks(inner, block) + 3) / 4; }
 
 // Offset of the scale byte of row r and block j; `groups` scale tiles per row of tiles.
-__host__ __device__ __forceinline__ int64_t fp4_scale_offset(int64_t r, int j, int64_t groups) {
-  return ((r >> 7) * groups + (j >> 2)) * kFp4TileBytes + (r & 31) * 16 + ((r >> 5) & 3) * 4 + (j & 3);
+__device__ __forceinline__ int64_t fp4_scale_offset(uint32_t r, int j, int groups) {
+  const uint32_t in_tile = (r & 31u) * 16u + ((r >> 5) & 3u) * 4u + ((uint32_t)j & 3u);
+  return (int64_t)((r >> 7) * (uint64_t)(uint32_t)groups + (uint32_t)(j >> 2)) * kFp4TileBytes + in_tile;
 }
 
 int check_fp4(const adaption_fp4tensor& t, int64_t inner);
@@ -43,16 +44,19 @@ int fp4_ip_impl(const Fp4Problem& p);
 
 inline int dtype_size(int32_t dtype) { return dtype == ADAPTION_F32 ? 4 : 2; }
 
-// Two numbers to E2M1 (nearest, ties to even, at most 6 in magnitude): `lo` in bits 0-3.
-__device__ __forceinline__ uint32_t fp4_pack2(float lo, float hi) {
+// Eight numbers to E2M1 (nearest, ties to even, at most 6 in magnitude), the first in bits 0-3.
+__device__ __forceinline__ uint32_t fp4_pack8(const float* v) {
   uint32_t r;
   asm("{\n"
-      ".reg .b8 b;\n"
-      "cvt.rn.satfinite.e2m1x2.f32 b, %2, %1;\n"
-      "cvt.u32.u8 %0, b;\n"
+      ".reg .b8 a, b, c, d;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
+      "mov.b32 %0, {a, b, c, d};\n"
       "}\n"
       : "=r"(r)
-      : "f"(lo), "f"(hi));
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
   return r;
 }
 // The two E2M1 numbers of a byte, bits 0-3 in the low half.
@@ -66,6 +70,12 @@ __device__ __forceinline__ __half2 fp4_unpack2(uint32_t byte) {
       : "=r"(r)
       : "r"(byte));
   return *reinterpret_cast<__half2*>(&r);
+}
+// 1 / v to one unit in the last place, for normal numbers
+__device__ __forceinline__ float reciprocal(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
 }
 // E4M3: the nearest of a number >= 0 (ties to even, at most 448), and the value of a byte.
 __device__ __forceinline__ uint32_t e4m3_nearest(float v) {

@@ -1,8 +1,7 @@
 // Microscaled 4-bit floating point: the quantizer and its inverse (adaption_fp4_quantize, adaption_fp4_dequantize).
 //
-// Both are one pass over memory.  A lane takes eight consecutive elements of a row (16 bytes of a 16-bit type, 4 bytes of
-// codes); the two or four lanes of a block find its maximum with shuffles, so that the values are read once and stay in
-// registers.
+// Both are one pass over memory.  A lane takes a chunk of 32 bytes of a row's real values (8 or 16 elements); the lanes of a
+// block, at most four, find its maximum with shuffles, so that the values are read once and stay in registers.
 //
 // Quantizer.  With amax the block's maximum:
 //   block 32: step 2^(floor(log2 amax) - 2).  The scale byte is amax's exponent field less 2 (a denormal amax has field 0,
@@ -11,14 +10,13 @@
 //     two codes.  The quotient is rounded to 32 bits before it is rounded to E2M1; that gives the nearest code
 //     all the same: a border m between two codes and the step have 3 and 4 significant bits, so m * step is a float, an x
 //     off that border is off by one unit in its last place at least, and that moves x / step by more than half a unit in m's last
-//     place (the step's significand is at most 1.875).  The division itself is q = x r, q += (x - q step) r with r the rounded reciprocal (Markstein, IBM J.
-//     Res. Dev. 34, 1990: the residual is exact in one fused multiply-add), three operations an element.  The same argument holds for
-//     amax / 6 against the borders of E4M3.
+//     place (the step's significand is at most 1.875).  The division itself is q = x r, q -= (q step - x) r with r the reciprocal
+//     to one unit in the last place (Markstein, IBM J. Res. Dev. 34, 1990): the residual is exact in one fused multiply-add, the
+//     correction leaves an error of 2^-44 before the last rounding, and an element costs three operations.  The same holds
+//     for amax / 6 against the borders of E4M3.
 #include "fp4.cuh"
 
 namespace adaption {
-
-int num_sms();
 
 int check_fp4(const adaption_fp4tensor& t, int64_t inner) {
   if (t.block != 16 && t.block != 32) return ADAPTION_ERR_INVALID_ARG;
@@ -38,10 +36,13 @@ int check_matrix(const adaption_matrix& m, int64_t inner) {
 
 namespace {
 
-constexpr int kVec = 8;              // elements of a lane
 constexpr int kThreads = 256;
+constexpr int kAhead = 2;            // chunks of a thread whose loads are in flight together
 
 enum Source { kF32 = ADAPTION_F32, kF16 = ADAPTION_F16, kBF16 = ADAPTION_BF16, kPlanes = 3 };
+
+// Elements of a chunk: what a lane takes at once, 32 bytes of x or of y.
+__host__ __device__ constexpr int chunk_of(int source) { return source == kF32 ? 8 : 16; }
 
 // Division of numbers below 2^30 by a fixed one below 2^30.
 struct Divider {
@@ -59,43 +60,163 @@ __device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& v) {
   return (uint32_t)(((uint64_t)n * v.mul) >> v.shift);
 }
 
+// 32 bytes, read once
+__device__ __forceinline__ void load_words(const void* at, bool aligned32, uint32_t (&w)[8]) {
+  if (aligned32) {
+    asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(at));
+  } else {
+    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(at)), b = __ldcs(reinterpret_cast<const uint4*>(at) + 1);
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+    w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  }
+}
+// The first `bytes` (at most 32) of what lies at an address of any alignment, from the aligned 16-byte words that hold
+// them: none of another word is touched.  What lies behind them is undefined.  (Element by element, rows off a 16-byte
+// boundary were read at a fifth of the speed.)
+__device__ __forceinline__ void load_shifted(const void* at, int bytes, uint32_t (&w)[8]) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(at);
+  const uint32_t sh = (uint32_t)a & 15u;
+  const uint4* q = reinterpret_cast<const uint4*>(a - sh);
+  uint32_t g[12];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    uint4 t = make_uint4(0u, 0u, 0u, 0u);
+    if (bytes > 0 && 16 * k < (int)sh + bytes) t = __ldg(q + k);
+    g[4 * k] = t.x; g[4 * k + 1] = t.y; g[4 * k + 2] = t.z; g[4 * k + 3] = t.w;
+  }
+  if (sh & 8u) {
+#pragma unroll
+    for (int k = 0; k < 10; ++k) g[k] = g[k + 2];
+  }
+  if (sh & 4u) {
+#pragma unroll
+    for (int k = 0; k < 9; ++k) g[k] = g[k + 1];
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) w[k] = sh & 2u ? __funnelshift_r(g[k], g[k + 1], 16) : g[k];
+}
+
+// Bytes of `a` by selector; one with bit 3 set is eight times the byte's sign.
+__device__ __forceinline__ uint32_t with_signs(uint32_t a, uint32_t selector) {
+  uint32_t r;
+  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(r) : "r"(a), "r"(selector));
+  return r;
+}
+
 struct QuantParams {
-  const void* x;                // real values, or the low plane
-  const int8_t* hi;             // high plane or null
-  int64_t stride;               // of a row of x, in elements
+  const uint8_t* x;             // real values, or the low plane
+  const uint8_t* hi;            // high plane or null
+  int64_t pitch;                // of a row of x (of a plane), in bytes
   float unit;                   // 2^-frac_bits of a fixed-point tensor
+  int aligned32;
   uint8_t* codes;
   uint8_t* scales;
   int64_t row_bytes;            // of the codes
-  int64_t groups;
-  uint32_t total;               // eight-element chunks of all rows
+  int groups;
+  uint32_t total;               // chunks of all rows
   Divider chunks;               // ... of one row
   int inner, c_stride, blocks4; // blocks4: blocks of a row, filled up to whole scale tiles
-  int exp, relu;
+  float inv_unit, step_unit;    // 2^-exp, 2^exp
+  int relu;
   adaption_stats* stats;
 };
 
-template <int SRC>
-__device__ __forceinline__ float load_one(const QuantParams& p, int64_t i) {
-  if (SRC == kF32) return reinterpret_cast<const float*>(p.x)[i];
-  if (SRC == kF16) return __half2float(reinterpret_cast<const __half*>(p.x)[i]);
-  if (SRC == kBF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p.x)[i]);
-  return (float)load_q(p.hi, reinterpret_cast<const uint8_t*>(p.x), (size_t)i) * p.unit;
+// The first n elements of a chunk as raw words (what lies behind them is undefined).
+template <int SRC, bool ALIGNED>
+__device__ __forceinline__ void load_chunk(const QuantParams& p, uint32_t row, int col, int n, uint32_t (&w)[8]) {
+  constexpr int kVec = chunk_of(SRC), kSize = SRC == kF32 ? 4 : 2;
+  if (SRC == kPlanes) {
+    // (planes are 16-byte aligned, pitches a multiple of 16, and cover their padding)
+    uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+    if (n > 0) {
+      lo = __ldcs(reinterpret_cast<const uint4*>(p.x + (int64_t)row * p.pitch + col));
+      if (p.hi != nullptr) hi = __ldcs(reinterpret_cast<const uint4*>(p.hi + (int64_t)row * p.pitch + col));
+    }
+    w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w;
+    w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+    return;
+  }
+  const uint8_t* at = p.x + (int64_t)row * p.pitch + (int64_t)col * kSize;
+  if (ALIGNED && n >= kVec)
+    load_words(at, p.aligned32 != 0, w);
+  else
+    load_shifted(at, min(n, kVec) * kSize, w);
 }
 
-// eight elements from i on, as one vector (two for 32-bit elements)
-template <int SRC>
-__device__ __forceinline__ void load_vector(const QuantParams& p, int64_t i, float (&v)[kVec]) {
-  if (SRC == kF32) {
-    const float4* q = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.x) + i);
-    const float4 a = __ldg(q), b = __ldg(q + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else if (SRC == kF16 || SRC == kBF16) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.x) + i));
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// Quantizes one chunk; every lane of the warp comes along (n = 0: nothing to quantize, but codes and scales of the padding).
+template <int SRC, int BLOCK>
+__device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, uint32_t row, int col, int n, uint32_t (&w)[8],
+                                               Counts& cnt) {
+  constexpr int kVec = chunk_of(SRC);
+  float v[kVec];
+  float top = 0.f;
+  if (SRC == kPlanes) {
+    // pairs of 16-bit integers from the planes' bytes (the sign repeated where there is one plane), their range, and each as
+    // a float: q + 2^15 behind the exponent of 2^23, less 2^23 + 2^15
+    uint32_t q[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 8; ++k) {
+      const uint32_t lo = w[k >> 1], hi = w[4 + (k >> 1)];
+      q[k] = p.hi != nullptr ? __byte_perm(lo, hi, k & 1 ? 0x7362 : 0x5140) : with_signs(lo, k & 1 ? 0xb3a2u : 0x9180u);
+    }
+    if (n < kVec) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) q[k] &= 2 * k + 1 < n ? 0xffffffffu : (2 * k < n ? 0xffffu : 0u);
+    }
+    uint32_t most = 0u, least = 0u;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (p.relu) q[k] = __vmaxs2(q[k], 0u);
+      most = __vmaxs2(most, q[k]);
+      least = __vmins2(least, q[k]);
+      q[k] ^= 0x80008000u;
+    }
+    int m = max(max((int)(int16_t)(most & 0xffffu), (int)most >> 16), -min((int)(int16_t)(least & 0xffffu), (int)least >> 16));
+#pragma unroll
+    for (int o = 1; o < BLOCK / kVec; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    top = (float)m * p.unit;
+    const float less = -8421376.f * p.unit;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      v[2 * k] = fmaf(__uint_as_float(__byte_perm(q[k], 0x4b000000u, 0x7610)), p.unit, less);
+      v[2 * k + 1] = fmaf(__uint_as_float(__byte_perm(q[k], 0x4b000000u, 0x7632)), p.unit, less);
+    }
+  } else if (SRC == kF32) {
+    uint32_t m = 0u;
+    if (n < kVec) {
+#pragma unroll
+      for (int k = 0; k < kVec; ++k)
+        if (k >= n) w[k] = 0u;
+    }
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+      if (p.relu) w[k] = (uint32_t)max((int32_t)w[k], 0);
+      m = max(m, w[k] & 0x7fffffffu);
+    }
+#pragma unroll
+    for (int o = 1; o < BLOCK / kVec; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) v[k] = __uint_as_float(w[k]);
+    top = __uint_as_float(m);
+  } else {
+    // magnitudes as 16-bit numbers, two at a time; relu: what has a sign is negative as a 16-bit number too
+    uint32_t m = 0u;
+    if (n < kVec) {
+#pragma unroll
+      for (int k = 0; k < kVec / 2; ++k) w[k] &= 2 * k + 1 < n ? 0xffffffffu : (2 * k < n ? 0xffffu : 0u);
+    }
+#pragma unroll
+    for (int k = 0; k < kVec / 2; ++k) {
+      if (p.relu) w[k] = __vmaxs2(w[k], 0u);
+      m = __vmaxu2(m, w[k] & 0x7fff7fffu);
+    }
+    m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+    for (int o = 1; o < BLOCK / kVec; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+    for (int k = 0; k < kVec / 2; ++k) {
       if (SRC == kF16) {
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
         v[2 * k] = f.x;
@@ -105,189 +226,279 @@ __device__ __forceinline__ void load_vector(const QuantParams& p, int64_t i, flo
         v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
       }
     }
-  } else {
-    const uint2 lo = __ldg(reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(p.x) + i));
-    if (p.hi != nullptr) {
-      const uint2 hi = __ldg(reinterpret_cast<const uint2*>(p.hi + i));
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        const uint32_t l = ((k < 4 ? lo.x : lo.y) >> (8 * (k & 3))) & 255u;
-        const int32_t h = (int32_t)((k < 4 ? hi.x : hi.y) << (24 - 8 * (k & 3))) >> 24;
-        v[k] = (float)(h * 256 + (int32_t)l) * p.unit;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = (float)((int32_t)((k < 4 ? lo.x : lo.y) << (24 - 8 * (k & 3))) >> 24) * p.unit;
-    }
+    top = SRC == kF16 ? __half2float(__ushort_as_half((unsigned short)m)) : __uint_as_float(m << 16);
   }
-}
-
-template <int SRC, int BLOCK, bool VEC>
-__global__ void __launch_bounds__(kThreads) fp4_quantize_kernel(const QuantParams p) {
-  pdl_prologue();
-  Counts cnt;
-  const uint32_t step = gridDim.x * kThreads;
-  // (whole warps take part in the shuffles; lanes behind the last chunk work on zeros)
-  for (uint32_t base = blockIdx.x * kThreads; base < p.total; base += step) {
-    const uint32_t t = base + threadIdx.x;
-    const bool real = t < p.total;
-    const uint32_t row = real ? divide(t, p.chunks) : 0u;
-    const int col = real ? (int)(t - row * p.chunks.d) * kVec : p.inner;
-    float v[kVec];
-    const int64_t at = (int64_t)row * p.stride + col;
-    if (VEC && col + kVec <= p.inner) {
-      load_vector<SRC>(p, at, v);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] = col + k < p.inner ? load_one<SRC>(p, at + k) : 0.f;
-    }
-    float top = 0.f;
+  if (SRC != kPlanes && !(top < __uint_as_float(0x7f800000u))) {
+    // a NaN or an infinity in the block: NaN -> 0, infinities -> the largest finite number, and the maximum again
+    // (the lanes of a block agree on it and come here together; those of another block need not)
+    constexpr int kLanes = BLOCK / kVec;
+    const uint32_t lanes = ((1u << kLanes) - 1u) << (threadIdx.x & 31u & ~(uint32_t)(kLanes - 1));
+    top = 0.f;
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
-      if (SRC != kPlanes) {
-        // NaN -> 0, infinities -> the largest finite number (fmaxf / fminf give the other operand for NaN)
-        v[k] = v[k] == v[k] ? fminf(fmaxf(v[k], -3.402823466e38f), 3.402823466e38f) : 0.f;
-      }
-      if (p.relu) v[k] = v[k] > 0.f ? v[k] : 0.f;
+      v[k] = v[k] == v[k] ? fminf(fmaxf(v[k], -3.402823466e38f), 3.402823466e38f) : 0.f;
       top = fmaxf(top, fabsf(v[k]));
     }
 #pragma unroll
-    for (int o = 1; o < BLOCK / kVec; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-
-    uint32_t byte;
-    if (BLOCK == 32) {
-      const int field = (int)(__float_as_uint(top) >> 23);
-      byte = (uint32_t)max(field - 2, 0);
-      const float inv = __uint_as_float((254u - byte) << 23);
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) v[k] *= inv;
-    } else {
-      byte = e4m3_nearest(__fdiv_rn(fminf(top * pow2_float(-p.exp), 3e38f), 6.f));
-      const float s = e4m3_value(byte) * pow2_float(p.exp);
-      const float r = s > 0.f ? __frcp_rn(s) : 0.f;
-      if (top > 8.f * s) {
-        // the largest scale was too small, or the smallest too large: beyond 8 steps all is clipped
-#pragma unroll
-        for (int k = 0; k < kVec; ++k) v[k] = fminf(fmaxf(v[k], -8.f * s), 8.f * s);
-      }
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        const float q = v[k] * r;
-        v[k] = copysignf(fmaf(fmaf(-q, s, v[k]), r, q), v[k]);
-      }
-    }
-    uint32_t code = 0;
-#pragma unroll
-    for (int k = 0; k < kVec / 2; ++k) code |= fp4_pack2(v[2 * k], v[2 * k + 1]) << (8 * k);
-    if (p.stats != nullptr) {
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        if (col + k < p.inner) {
-          cnt.zeros += ((code >> (4 * k)) & 7u) == 0u;
-          cnt.sat_pos += v[k] >= 7.f;
-          cnt.sat_neg += v[k] <= -7.f;
-        }
-      }
-    }
-    if (real && col < p.c_stride) *reinterpret_cast<uint32_t*>(p.codes + (int64_t)row * p.row_bytes + (col >> 1)) = code;
-    const int j = col / BLOCK;
-    if (real && (col & (BLOCK - 1)) == 0 && j < p.blocks4) p.scales[fp4_scale_offset(row, j, p.groups)] = (uint8_t)byte;
+    for (int o = 1; o < BLOCK / kVec; o <<= 1) top = fmaxf(top, __shfl_xor_sync(lanes, top, o));
   }
+
+  uint32_t byte;
+  if (BLOCK == 32) {
+    byte = (uint32_t)max((int)(__float_as_uint(top) >> 23) - 2, 0);
+    const float inv = __uint_as_float((254u - byte) << 23);
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) v[k] *= inv;
+  } else {
+    const float t = fminf(top * p.inv_unit, 3e38f), sixth = 1.f / 6.f, t6 = t * sixth;
+    byte = e4m3_nearest(fmaf(fmaf(t6, 6.f, -t), -sixth, t6));
+    const float s = e4m3_value(byte) * p.step_unit;
+    const float r = s > 0.f ? reciprocal(s) : 0.f;
+    if (top > 8.f * s) {
+      // the largest scale was too small, or the smallest too large: beyond 8 steps all is clipped
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) v[k] = fminf(fmaxf(v[k], -8.f * s), 8.f * s);
+    }
+    // (in this form a zero keeps its sign)
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+      const float q = v[k] * r;
+      v[k] = fmaf(fmaf(q, s, -v[k]), -r, q);
+    }
+  }
+  uint32_t code[kVec / 8];
+#pragma unroll
+  for (int i = 0; i < kVec / 8; ++i) code[i] = fp4_pack8(v + 8 * i);
+  if (p.stats != nullptr) {
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+      if (k < n) {
+        cnt.zeros += ((code[k >> 3] >> (4 * (k & 7))) & 7u) == 0u;
+        cnt.sat_pos += v[k] >= 7.f;
+        cnt.sat_neg += v[k] <= -7.f;
+      }
+    }
+  }
+  if (real) {
+    uint8_t* to = p.codes + (int64_t)row * p.row_bytes + (col >> 1);
+    if (kVec == 16) *reinterpret_cast<uint2*>(to) = make_uint2(code[0], code[kVec / 8 - 1]);
+    else *reinterpret_cast<uint32_t*>(to) = code[0];
+  }
+  const int j = col / BLOCK;
+  if (real && (col & (BLOCK - 1)) == 0 && j < p.blocks4) {
+    uint8_t* const to = p.scales + fp4_scale_offset(row, j, p.groups);
+    *to = (uint8_t)byte;
+    // the last block of the pitch: zeros in the rest of the scale tile
+    if (col + BLOCK >= p.c_stride)
+      for (int k = 1; j + k < p.blocks4; ++k) to[k] = 0;
+  }
+}
+
+template <int SRC, int BLOCK, bool ALIGNED>
+__global__ void __launch_bounds__(kThreads) fp4_quantize_kernel(const QuantParams p) {
+  pdl_prologue();
+  constexpr int kVec = chunk_of(SRC);
+  Counts cnt;
+  uint32_t w[kAhead][8], row[kAhead];
+  int col[kAhead];
+  bool real[kAhead];
+  const uint32_t base = blockIdx.x * (kThreads * kAhead) + threadIdx.x;
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const uint32_t t = base + u * kThreads;
+    real[u] = t < p.total;
+    row[u] = real[u] ? divide(t, p.chunks) : 0u;
+    col[u] = real[u] ? (int)(t - row[u] * p.chunks.d) * kVec : 0;
+    load_chunk<SRC, ALIGNED>(p, row[u], col[u], real[u] ? p.inner - col[u] : 0, w[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u)
+    quantize_chunk<SRC, BLOCK>(p, real[u], row[u], col[u], real[u] ? p.inner - col[u] : 0, w[u], cnt);
   if (p.stats != nullptr) flush_counts_block(cnt, p.stats);
 }
 
 struct ValueParams {
   const uint8_t* codes;
   const uint8_t* scales;
-  int64_t row_bytes, groups;
+  int64_t row_bytes;
+  int groups;
   uint32_t total;
   Divider chunks;
   int inner;
   float unit;                   // 2^exp
-  void* y;
-  int64_t stride;
+  int aligned32;
+  uint8_t* y;
+  int64_t pitch;                // of a row of y, in bytes
 };
 
+// two values as one word of a 16-bit type
 template <int DT>
-__device__ __forceinline__ void store_one(void* y, int64_t i, float v) {
-  if (DT == kF32) reinterpret_cast<float*>(y)[i] = v;
-  else if (DT == kF16) reinterpret_cast<__half*>(y)[i] = __float2half_rn(v);
-  else reinterpret_cast<__nv_bfloat16*>(y)[i] = __float2bfloat16_rn(v);
+__device__ __forceinline__ uint32_t pack_values(float a, float b) {
+  if (DT == kF16) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <int BLOCK>
+__device__ __forceinline__ float step_of(const ValueParams& p, uint32_t byte) {
+  return BLOCK == 32 ? e8m0_value(byte) : e4m3_value(byte) * p.unit;
 }
 
-template <int DT, int BLOCK, bool VEC>
+// Rows of y on 16-byte boundaries: a lane takes a chunk of codes, which lies in one block.
+template <int DT, int BLOCK>
 __global__ void __launch_bounds__(kThreads) fp4_values_kernel(const ValueParams p) {
   pdl_prologue();
-  const uint32_t step = gridDim.x * kThreads;
-  for (uint32_t t = blockIdx.x * kThreads + threadIdx.x; t < p.total; t += step) {
-    const uint32_t row = divide(t, p.chunks);
-    const int col = (int)(t - row * p.chunks.d) * kVec;
-    const uint32_t code = __ldg(reinterpret_cast<const uint32_t*>(p.codes + (int64_t)row * p.row_bytes + (col >> 1)));
-    const uint32_t byte = __ldg(p.scales + fp4_scale_offset(row, col / BLOCK, p.groups));
-    const float s = BLOCK == 32 ? e8m0_value(byte) : e4m3_value(byte) * p.unit;
-    float v[kVec];
+  constexpr int kVec = chunk_of(DT);
+  uint32_t code[kAhead][kVec / 8], byte[kAhead], row[kAhead];
+  int col[kAhead];
+  const uint32_t base = blockIdx.x * (kThreads * kAhead) + threadIdx.x;
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const uint32_t t = base + u * kThreads;
+    row[u] = t < p.total ? divide(t, p.chunks) : 0u;
+    col[u] = t < p.total ? (int)(t - row[u] * p.chunks.d) * kVec : p.inner;
+    if (col[u] < p.inner) {
+      const uint8_t* at = p.codes + (int64_t)row[u] * p.row_bytes + (col[u] >> 1);
+      if (kVec == 16) {
+        const uint2 c = __ldg(reinterpret_cast<const uint2*>(at));
+        code[u][0] = c.x;
+        code[u][kVec / 8 - 1] = c.y;
+      } else {
+        code[u][0] = __ldg(reinterpret_cast<const uint32_t*>(at));
+      }
+      byte[u] = __ldg(p.scales + fp4_scale_offset(row[u], col[u] / BLOCK, p.groups));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const int n = p.inner - col[u];
+    if (n <= 0) continue;
+    const float s = step_of<BLOCK>(p, byte[u]);
+    uint32_t w[8];
 #pragma unroll
     for (int k = 0; k < kVec / 2; ++k) {
-      const float2 f = __half22float2(fp4_unpack2((code >> (8 * k)) & 255u));
-      v[2 * k] = f.x * s;
-      v[2 * k + 1] = f.y * s;
-    }
-    const int64_t at = (int64_t)row * p.stride + col;
-    if (VEC && col + kVec <= p.inner) {
+      const float2 f = __half22float2(fp4_unpack2((code[u][k >> 2] >> (8 * (k & 3))) & 255u));
       if (DT == kF32) {
-        float4* q = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + at);
-        q[0] = make_float4(v[0], v[1], v[2], v[3]);
-        q[1] = make_float4(v[4], v[5], v[6], v[7]);
+        w[2 * k & 7] = __float_as_uint(f.x * s);
+        w[(2 * k + 1) & 7] = __float_as_uint(f.y * s);
       } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (DT == kF16) {
-            const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-            w[k] = *reinterpret_cast<const uint32_t*>(&h);
-          } else {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-            w[k] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-        }
-        *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p.y) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+        w[k] = pack_values<DT>(f.x * s, f.y * s);
+      }
+    }
+    uint8_t* to = p.y + (int64_t)row[u] * p.pitch + (int64_t)col[u] * (DT == kF32 ? 4 : 2);
+    if (n >= kVec) {
+      if (p.aligned32) {
+        asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                     "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+      } else {
+        __stcs(reinterpret_cast<uint4*>(to), make_uint4(w[0], w[1], w[2], w[3]));
+        __stcs(reinterpret_cast<uint4*>(to) + 1, make_uint4(w[4], w[5], w[6], w[7]));
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < kVec; ++k)
-        if (col + k < p.inner) store_one<DT>(p.y, at + k, v[k]);
+      for (int k = 0; k < kVec; ++k) {
+        if (k >= n) break;
+        if (DT == kF32) reinterpret_cast<uint32_t*>(to)[k] = w[k & 7];
+        else reinterpret_cast<uint16_t*>(to)[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+      }
     }
   }
 }
 
-int grid_for(uint32_t total) {
-  const int64_t blocks = ((int64_t)total + kThreads - 1) / kThreads, most = (int64_t)num_sms() * 8;
-  return (int)(blocks < most ? blocks : most);
+// Rows of y anywhere: a lane takes an aligned 32-byte piece of y, whose elements start anywhere in a byte of codes and in a
+// block.  `chunks` counts the pieces that a row can touch.
+template <int DT, int BLOCK>
+__global__ void __launch_bounds__(kThreads) fp4_values_shifted_kernel(const ValueParams p) {
+  pdl_prologue();
+  constexpr int kVec = chunk_of(DT), kSize = 32 / kVec, kWords = kVec / 8;
+  uint32_t code[kAhead][kWords + 1], byte0[kAhead], byte1[kAhead];
+  int c0[kAhead], c1[kAhead];              // first and last element of the piece that exist
+  uint8_t* to[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const uint32_t t = blockIdx.x * (kThreads * kAhead) + u * kThreads + threadIdx.x;
+    const uint32_t row = t < p.total ? divide(t, p.chunks) : 0u;
+    uint8_t* const y = p.y + (int64_t)row * p.pitch;
+    const int off = (int)(reinterpret_cast<uintptr_t>(y) & 31u) / kSize;
+    const int col = (int)(t - row * p.chunks.d) * kVec - off;         // negative: the piece begins before the row
+    c0[u] = max(col, 0);
+    c1[u] = t < p.total ? min(col + kVec, p.inner) - 1 : -1;
+    to[u] = y + (int64_t)c0[u] * kSize;
+    if (c0[u] <= c1[u]) {
+      const uint32_t* const codes = reinterpret_cast<const uint32_t*>(p.codes + (int64_t)row * p.row_bytes);
+      const int first = c0[u] >> 3, last = c1[u] >> 3;
+#pragma unroll
+      for (int i = 0; i <= kWords; ++i) code[u][i] = first + i <= last ? __ldg(codes + first + i) : 0u;
+      const int j0 = c0[u] / BLOCK, j1 = c1[u] / BLOCK;
+      byte0[u] = __ldg(p.scales + fp4_scale_offset(row, j0, p.groups));
+      byte1[u] = j1 == j0 ? byte0[u] : __ldg(p.scales + fp4_scale_offset(row, j1, p.groups));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const int n = c1[u] - c0[u] + 1;
+    if (n <= 0) continue;
+    const float s0 = step_of<BLOCK>(p, byte0[u]), s1 = step_of<BLOCK>(p, byte1[u]);
+    const int border = c1[u] / BLOCK * BLOCK - c0[u];                 // elements from here on lie in the second block
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const uint32_t eight = __funnelshift_r(code[u][i], code[u][i + 1], 4 * (c0[u] & 7));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int e = 8 * i + 2 * k;
+        const float2 f = __half22float2(fp4_unpack2((eight >> (8 * k)) & 255u));
+        const float a = f.x * (e < border ? s0 : s1), b = f.y * (e + 1 < border ? s0 : s1);
+        if (DT == kF32) {
+          w[e & 7] = __float_as_uint(a);
+          w[(e + 1) & 7] = __float_as_uint(b);
+        } else {
+          w[e >> 1] = pack_values<DT>(a, b);
+        }
+      }
+    }
+    if (n == kVec) {
+      __stcs(reinterpret_cast<uint4*>(to[u]), make_uint4(w[0], w[1], w[2], w[3]));
+      __stcs(reinterpret_cast<uint4*>(to[u]) + 1, make_uint4(w[4], w[5], w[6], w[7]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) {
+        if (k >= n) break;
+        if (DT == kF32) reinterpret_cast<uint32_t*>(to[u])[k] = w[k & 7];
+        else reinterpret_cast<uint16_t*>(to[u])[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+      }
+    }
+  }
 }
 
+unsigned blocks_of(uint32_t total, int per_block) { return (total + (uint32_t)per_block - 1) / (uint32_t)per_block; }
+
 template <int SRC, int BLOCK>
-int launch_quantize(const QuantParams& p, bool vec, cudaStream_t stream) {
-  const dim3 grid(grid_for(p.total));
-  return cuda_status(vec ? launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, true>, grid, dim3(kThreads), stream, p)
-                         : launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, false>, grid, dim3(kThreads), stream, p),
+int launch_quantize(const QuantParams& p, bool aligned, cudaStream_t stream) {
+  const dim3 grid(blocks_of(p.total, kThreads * kAhead)), block(kThreads);
+  return cuda_status(aligned || SRC == kPlanes
+                         ? launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, true>, grid, block, stream, p)
+                         : launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, false>, grid, block, stream, p),
                      "fp4_quantize_kernel launch");
 }
 template <int SRC>
-int launch_quantize(const QuantParams& p, int block, bool vec, cudaStream_t stream) {
-  return block == 32 ? launch_quantize<SRC, 32>(p, vec, stream) : launch_quantize<SRC, 16>(p, vec, stream);
+int launch_quantize(const QuantParams& p, int block, bool aligned, cudaStream_t stream) {
+  return block == 32 ? launch_quantize<SRC, 32>(p, aligned, stream) : launch_quantize<SRC, 16>(p, aligned, stream);
 }
 
+template <int DT, int BLOCK>
+int launch_values(const ValueParams& p, bool aligned, cudaStream_t stream) {
+  const dim3 grid(blocks_of(p.total, kThreads * kAhead)), block(kThreads);
+  return cuda_status(aligned ? launch_after_predecessor(fp4_values_kernel<DT, BLOCK>, grid, block, stream, p)
+                             : launch_after_predecessor(fp4_values_shifted_kernel<DT, BLOCK>, grid, block, stream, p),
+                     "fp4_values_kernel launch");
+}
 template <int DT>
-int launch_values(const ValueParams& p, int block, bool vec, cudaStream_t stream) {
-  const dim3 grid(grid_for(p.total));
-  cudaError_t e;
-  if (block == 32)
-    e = vec ? launch_after_predecessor(fp4_values_kernel<DT, 32, true>, grid, dim3(kThreads), stream, p)
-            : launch_after_predecessor(fp4_values_kernel<DT, 32, false>, grid, dim3(kThreads), stream, p);
-  else
-    e = vec ? launch_after_predecessor(fp4_values_kernel<DT, 16, true>, grid, dim3(kThreads), stream, p)
-            : launch_after_predecessor(fp4_values_kernel<DT, 16, false>, grid, dim3(kThreads), stream, p);
-  return cuda_status(e, "fp4_values_kernel launch");
+int launch_values(const ValueParams& p, int block, bool aligned, cudaStream_t stream) {
+  return block == 32 ? launch_values<DT, 32>(p, aligned, stream) : launch_values<DT, 16>(p, aligned, stream);
 }
 
 // Rows per launch: chunks are counted below 2^29.  A multiple of a scale tile's rows.
@@ -312,25 +523,25 @@ int fp4_quantize_impl(const adaption_matrix& x, const adaption_qtensor* q, size_
   p.inner = (int)inner;
   p.c_stride = (int)out.c_stride;
   p.row_bytes = out.c_stride / 2;
-  p.groups = fp4_groups((int64_t)inner, out.block);
-  p.blocks4 = (int)p.groups * 4;
-  p.exp = out.exp;
+  p.groups = (int)fp4_groups((int64_t)inner, out.block);
+  p.blocks4 = p.groups * 4;
+  p.inv_unit = pow2_float(-out.exp);
+  p.step_unit = pow2_float(out.exp);
   p.relu = relu ? 1 : 0;
   p.stats = stats;
-  const int64_t width = out.c_stride > (int64_t)p.blocks4 * out.block ? out.c_stride : (int64_t)p.blocks4 * out.block;
-  p.chunks = make_divider((uint32_t)(width / kVec));
-  bool vec = true;
-  int64_t item = 1;
+  const int vec = chunk_of(q != nullptr ? (int)kPlanes : x.dtype);
+  p.chunks = make_divider((uint32_t)(out.c_stride / vec));
+  bool aligned = true;
   if (q != nullptr) {
-    p.x = q->lo;
-    p.hi = q->fmt.n_bits > 8 ? (const int8_t*)q->hi : nullptr;
-    p.stride = q->c_stride;
+    p.x = (const uint8_t*)q->lo;
+    p.hi = q->fmt.n_bits > 8 ? (const uint8_t*)q->hi : nullptr;
+    p.pitch = q->c_stride;
     p.unit = pow2_float(-q->fmt.frac_bits);
   } else {
-    p.x = x.data;
-    p.stride = x.stride;
-    item = dtype_size(x.dtype);
-    vec = aligned16(x.data) && ((x.stride * item) & 15) == 0;
+    p.x = (const uint8_t*)x.data;
+    p.pitch = x.stride * dtype_size(x.dtype);
+    aligned = aligned16(x.data) && (p.pitch & 15) == 0;
+    p.aligned32 = ((reinterpret_cast<uintptr_t>(x.data) | (uintptr_t)p.pitch) & 31u) == 0;
   }
   p.codes = (uint8_t*)out.codes;
   p.scales = (uint8_t*)out.scales;
@@ -338,15 +549,15 @@ int fp4_quantize_impl(const adaption_matrix& x, const adaption_qtensor* q, size_
   for (int64_t r = 0; r < (int64_t)outer; r += rows) {
     const int64_t n = (int64_t)outer - r < rows ? (int64_t)outer - r : rows;
     p.total = (uint32_t)(n * p.chunks.d);
-    if (q != nullptr) rc = launch_quantize<kPlanes>(p, out.block, vec, stream);
-    else if (x.dtype == ADAPTION_F32) rc = launch_quantize<kF32>(p, out.block, vec, stream);
-    else if (x.dtype == ADAPTION_F16) rc = launch_quantize<kF16>(p, out.block, vec, stream);
-    else rc = launch_quantize<kBF16>(p, out.block, vec, stream);
+    if (q != nullptr) rc = launch_quantize<kPlanes>(p, out.block, aligned, stream);
+    else if (x.dtype == ADAPTION_F32) rc = launch_quantize<kF32>(p, out.block, aligned, stream);
+    else if (x.dtype == ADAPTION_F16) rc = launch_quantize<kF16>(p, out.block, aligned, stream);
+    else rc = launch_quantize<kBF16>(p, out.block, aligned, stream);
     if (rc != ADAPTION_OK) return rc;
-    p.x = (const uint8_t*)p.x + n * p.stride * item;
-    if (p.hi != nullptr) p.hi += n * p.stride;
+    p.x += n * p.pitch;
+    if (p.hi != nullptr) p.hi += n * p.pitch;
     p.codes += n * p.row_bytes;
-    p.scales += n / kFp4TileRows * p.groups * kFp4TileBytes;
+    p.scales += n / kFp4TileRows * (int64_t)p.groups * kFp4TileBytes;
   }
   return ADAPTION_OK;
 }
@@ -362,26 +573,28 @@ int fp4_dequantize_impl(const adaption_fp4tensor& x, size_t outer, size_t inner,
   ValueParams p{};
   p.inner = (int)inner;
   p.row_bytes = x.c_stride / 2;
-  p.groups = fp4_groups((int64_t)inner, x.block);
-  p.chunks = make_divider((uint32_t)((inner + kVec - 1) / kVec));
+  p.groups = (int)fp4_groups((int64_t)inner, x.block);
   p.unit = pow2_float(x.exp);
   p.codes = (const uint8_t*)x.codes;
   p.scales = (const uint8_t*)x.scales;
-  p.y = y.data;
-  p.stride = y.stride;
-  const int64_t item = dtype_size(y.dtype);
-  const bool vec = aligned16(y.data) && ((y.stride * item) & 15) == 0;
+  p.y = (uint8_t*)y.data;
+  p.pitch = y.stride * dtype_size(y.dtype);
+  const bool aligned = aligned16(y.data) && (p.pitch & 15) == 0;
+  p.aligned32 = ((reinterpret_cast<uintptr_t>(y.data) | (uintptr_t)p.pitch) & 31u) == 0;
+  const int64_t vec = chunk_of(y.dtype);
+  // (a row off the boundary can touch one piece more)
+  p.chunks = make_divider((uint32_t)(((int64_t)inner + vec - 1) / vec + (aligned ? 0 : 1)));
   const int64_t rows = rows_per_launch(p.chunks.d);
   for (int64_t r = 0; r < (int64_t)outer; r += rows) {
     const int64_t n = (int64_t)outer - r < rows ? (int64_t)outer - r : rows;
     p.total = (uint32_t)(n * p.chunks.d);
-    if (y.dtype == ADAPTION_F32) rc = launch_values<kF32>(p, x.block, vec, stream);
-    else if (y.dtype == ADAPTION_F16) rc = launch_values<kF16>(p, x.block, vec, stream);
-    else rc = launch_values<kBF16>(p, x.block, vec, stream);
+    if (y.dtype == ADAPTION_F32) rc = launch_values<kF32>(p, x.block, aligned, stream);
+    else if (y.dtype == ADAPTION_F16) rc = launch_values<kF16>(p, x.block, aligned, stream);
+    else rc = launch_values<kBF16>(p, x.block, aligned, stream);
     if (rc != ADAPTION_OK) return rc;
     p.codes += n * p.row_bytes;
-    p.scales += n / kFp4TileRows * p.groups * kFp4TileBytes;
-    p.y = (uint8_t*)p.y + n * p.stride * item;
+    p.scales += n / kFp4TileRows * (int64_t)p.groups * kFp4TileBytes;
+    p.y += n * p.pitch;
   }
   return ADAPTION_OK;
 }
