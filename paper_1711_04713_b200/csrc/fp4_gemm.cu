@@ -17,9 +17,8 @@
 
 #include <cstring>
 
-#include "fp4.cuh"
+#include "fp4_mma.cuh"
 #include "knobs.cuh"
-#include "tc_ptx.cuh"
 #include "tensor_maps.cuh"
 
 namespace adaption {
@@ -28,13 +27,8 @@ int num_sms();
 
 namespace {
 
-constexpr int kRows = 128;                 // output channels of a tile
-constexpr int kBlockBytes = 128;           // codes of a k-block and row
-constexpr int kBlockElems = 256;
-constexpr int kStepElems = 64;             // of one MMA
 constexpr int kMaxStages = 10;
 constexpr int kThreads = 256;              // warp 0: copies; 1: MMA; all of them: the epilogue
-constexpr uint32_t kABytes = kRows * kBlockBytes;
 
 struct FpParams {
   int O, B;                     // output channels, batch rows
@@ -87,51 +81,6 @@ __device__ __forceinline__ bool fp_wait(uint32_t bar, uint32_t parity, FpCtrl* c
   return fp_wait_slow(bar, parity, ctrl, p);
 }
 
-// contiguous bytes of global memory -> this CTA's shared memory
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(bar)
-               : "memory");
-}
-// One scale tile (32 rows of 16 bytes) from shared memory to four TMEM columns, repeated in all lane quarters.
-__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t desc_lo, uint32_t desc_hi) {
-  asm volatile(
-      "{\n"
-      ".reg .b64 d;\n"
-      "mov.b64 d, {%1, %2};\n"
-      "tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], d;\n"
-      "}\n" ::"r"(taddr),
-      "r"(desc_lo), "r"(desc_hi)
-      : "memory");
-}
-template <int BLOCK>
-__device__ __forceinline__ void mma_fp4(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
-                                        uint32_t sfb, uint32_t accumulate) {
-#define ADAPTION_MMA_FP4(KIND)                                                                     \
-  asm volatile(                                                                                    \
-      "{\n"                                                                                        \
-      ".reg .pred p;\n"                                                                            \
-      ".reg .b64 da, db;\n"                                                                        \
-      "setp.ne.b32 p, %5, 0;\n"                                                                    \
-      "mov.b64 da, {%1, %3};\n"                                                                    \
-      "mov.b64 db, {%2, %3};\n"                                                                    \
-      "tcgen05.mma.cta_group::1." KIND " [%0], da, db, %4, [%6], [%7], p;\n"                       \
-      "}\n" ::"r"(d),                                                                              \
-      "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)          \
-      : "memory")
-  if (BLOCK == 32)
-    ADAPTION_MMA_FP4("kind::mxf4.block_scale.scale_vec::2X");
-  else
-    ADAPTION_MMA_FP4("kind::mxf4nvf4.block_scale.scale_vec::4X");
-#undef ADAPTION_MMA_FP4
-}
-// Instruction descriptor: E2M1 operands, both K-major, scales E8M0 (blocks of 32) or E4M3.
-__device__ __forceinline__ uint32_t make_idesc_fp4(int block, int n, int m) {
-  return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((block == 32 ? 1u : 0u) << 23) | ((uint32_t)(m >> 4) << 24);
-}
-// ... which two of the four scales of a TMEM word an instruction takes (blocks of 32): bytes 2 * half on
-__device__ __forceinline__ uint32_t scale_half(uint32_t half) { return (half * 2u) << 4 | (half * 2u) << 29; }
-
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
@@ -177,7 +126,7 @@ __device__ __forceinline__ void store_outputs(const FpParams& p, long long at, c
 template <int BLOCK>
 __global__ void __launch_bounds__(kThreads, 1)
 fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const FpParams p) {
-  constexpr int kGroups = BLOCK == 32 ? 2 : 4;             // scale tiles of a k-block and 128 rows
+  constexpr int kGroups = groups_of(BLOCK);
   extern __shared__ uint8_t smem_raw[];
   __shared__ FpCtrl ctrl;
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -271,13 +220,13 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       const uint32_t ta = tmem + p.sf_col + (uint32_t)s * slot, tbx = ta + 4u * kGroups;
       if (elect_one()) {
         for (int g = 0; g < groups; ++g) {
-          scales_to_tmem(ta + 4u * g, sf + 32u * g, shi);
+          scales_to_tmem<false>(ta + 4u * g, sf + 32u * g, shi);
           for (int c = 0; c < p.chunks_b; ++c)
-            scales_to_tmem(tbx + cols_b * g + 4u * c, sf + 32u * (uint32_t)((1 + c) * kGroups + g), shi);
+            scales_to_tmem<false>(tbx + cols_b * g + 4u * c, sf + 32u * (uint32_t)((1 + c) * kGroups + g), shi);
         }
         for (int k = 0; k < steps; ++k) {
           const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
-          mma_fp4<BLOCK>(tmem, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g,
+          mma_fp4<BLOCK, false>(tmem, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g,
                          tbx + cols_b * g, (kb > kb_begin || k > 0) ? 1u : 0u);
         }
         tc_commit<false>(smem_u32(&ctrl.empty[s]));
@@ -391,8 +340,8 @@ int launch_cluster_fp4(const CUtensorMap& ma, const CUtensorMap& mb, const FpPar
 
 }  // namespace
 
-int fp4_ip_impl(const Fp4Problem& g) {
-  const int block = g.w.block, kgroups = block == 32 ? 2 : 4;
+static int launch_fp4_cluster(const Fp4Problem& g) {
+  const int block = g.w.block, kgroups = groups_of(block);
   FpParams p;
   std::memset(&p, 0, sizeof(p));
   p.O = (int)g.O;
@@ -450,6 +399,10 @@ int fp4_ip_impl(const Fp4Problem& g) {
   const int grid = (int)(tiles * p.S);
   return block == 32 ? launch_cluster_fp4<32>(ma, mb, p, grid, smem, g.stream)
                      : launch_cluster_fp4<16>(ma, mb, p, grid, smem, g.stream);
+}
+
+int fp4_ip_impl(const Fp4Problem& g) {
+  return fp4_pair_preferred(g) ? launch_fp4_pair(g) : launch_fp4_cluster(g);
 }
 
 }  // namespace adaption

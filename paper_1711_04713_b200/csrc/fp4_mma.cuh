@@ -1,0 +1,84 @@
+// Building blocks of the products of microscaled 4-bit operands: scale copies to TMEM, block-scaled MMA, outputs.
+#pragma once
+
+#include "fp4.cuh"
+#include "tc_ptx.cuh"
+
+namespace adaption {
+namespace {
+
+constexpr int kRows = 128;                 // output channels of a CTA's tile
+constexpr int kBlockBytes = 128;           // codes of a k-block and row
+constexpr int kBlockElems = 256;
+constexpr int kStepElems = 64;             // of one MMA
+constexpr uint32_t kABytes = kRows * kBlockBytes;
+
+__host__ __device__ constexpr int groups_of(int block) { return block == 32 ? 2 : 4; }    // scale tiles of a k-block and 128 rows
+
+// contiguous bytes of global memory -> this CTA's shared memory
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+// One scale tile (32 rows of 16 bytes) from shared memory to four TMEM columns, repeated in all lane quarters.  PAIR: in both
+// CTAs, each from its own shared memory.
+template <bool PAIR>
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t desc_lo, uint32_t desc_hi) {
+#define ADAPTION_SCALES(CG)                                    \
+  asm volatile(                                                \
+      "{\n"                                                    \
+      ".reg .b64 d;\n"                                         \
+      "mov.b64 d, {%1, %2};\n"                                 \
+      "tcgen05.cp.cta_group::" CG ".32x128b.warpx4 [%0], d;\n" \
+      "}\n" ::"r"(taddr),                                      \
+      "r"(desc_lo), "r"(desc_hi)                               \
+      : "memory")
+  if (PAIR)
+    ADAPTION_SCALES("2");
+  else
+    ADAPTION_SCALES("1");
+#undef ADAPTION_SCALES
+}
+template <int BLOCK, bool PAIR>
+__device__ __forceinline__ void mma_fp4(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
+                                        uint32_t sfb, uint32_t accumulate) {
+#define ADAPTION_MMA_FP4(CG, KIND)                                                                  \
+  asm volatile(                                                                                    \
+      "{\n"                                                                                        \
+      ".reg .pred p;\n"                                                                            \
+      ".reg .b64 da, db;\n"                                                                        \
+      "setp.ne.b32 p, %5, 0;\n"                                                                    \
+      "mov.b64 da, {%1, %3};\n"                                                                    \
+      "mov.b64 db, {%2, %3};\n"                                                                    \
+      "tcgen05.mma.cta_group::" CG "." KIND " [%0], da, db, %4, [%6], [%7], p;\n"                  \
+      "}\n" ::"r"(d),                                                                              \
+      "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)          \
+      : "memory")
+  if (BLOCK == 32 && PAIR)
+    ADAPTION_MMA_FP4("2", "kind::mxf4.block_scale.scale_vec::2X");
+  else if (BLOCK == 32)
+    ADAPTION_MMA_FP4("1", "kind::mxf4.block_scale.scale_vec::2X");
+  else if (PAIR)
+    ADAPTION_MMA_FP4("2", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+  else
+    ADAPTION_MMA_FP4("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+#undef ADAPTION_MMA_FP4
+}
+// Instruction descriptor: E2M1 operands, both K-major, scales E8M0 (blocks of 32) or E4M3.
+__device__ __forceinline__ uint32_t make_idesc_fp4(int block, int n, int m) {
+  return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((block == 32 ? 1u : 0u) << 23) | ((uint32_t)(m >> 4) << 24);
+}
+// ... which two of the four scales of a TMEM word an instruction takes (blocks of 32): bytes 2 * half on
+__device__ __forceinline__ uint32_t scale_half(uint32_t half) { return (half * 2u) << 4 | (half * 2u) << 29; }
+
+
+template <int DT>
+__device__ __forceinline__ void store_output(void* y, long long at, float v) {
+  if (DT == ADAPTION_F32) reinterpret_cast<float*>(y)[at] = v;
+  else if (DT == ADAPTION_F16) reinterpret_cast<__half*>(y)[at] = __float2half_rn(v);
+  else reinterpret_cast<__nv_bfloat16*>(y)[at] = __float2bfloat16_rn(v);
+}
+
+}  // namespace
+}  // namespace adaption

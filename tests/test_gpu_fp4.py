@@ -192,13 +192,20 @@ def check_product(y, xv, wv, bias, relu, block, dtype, cols=None):
     assert np.all(err <= bound), (float((err / np.maximum(bound, 1e-300)).max()), np.argwhere(err > bound)[:5].tolist())
 
 
+def choose(kernel):
+    """One cluster of CTAs per tile, or the persistent kernel over pairs of CTAs, wherever the call would run."""
+    B.adaption_debug_set("pair", {"cluster": 0, "pair": 1}[kernel])
+
+
 IP_SHAPES = [(1, 1, 1), (1, 64, 128), (1, 4096, 300), (5, 300, 130), (16, 257, 129), (17, 1000, 64), (64, 2048, 256), (100, 33, 500),
              (128, 512, 128), (129, 640, 140), (200, 1411, 257), (256, 768, 200), (257, 256, 128), (300, 900, 384), (520, 320, 1000)]
 
 
+@pytest.mark.parametrize("kernel", ["cluster", "pair"])
 @pytest.mark.parametrize("block", [16, 32])
 @pytest.mark.parametrize("shape", IP_SHAPES)
-def test_inner_product(shape, block):
+def test_inner_product(shape, block, kernel):
+    choose(kernel)
     Bn, K, O = shape
     rng = np.random.default_rng(Bn + K + O)
     ex, ew = (-3, 2) if block == 16 else (0, 0)
@@ -217,10 +224,12 @@ def test_inner_product(shape, block):
         assert s.status == 0 and s.zeros == int((y == 0).sum())
 
 
+@pytest.mark.parametrize("kernel", ["cluster", "pair"])
 @pytest.mark.parametrize("block", [16, 32])
-def test_inner_product_of_exact_sums(block):
+def test_inner_product_of_exact_sums(block, kernel):
     """Steps of 1 (and of 2 and 1/2): every partial sum is a multiple of 1/16 below 2^20, so the result is exact, and
     any element taken from a wrong place, or with a wrong scale, shows."""
+    choose(kernel)
     one = 127 if block == 32 else 56
     for Bn, K, O in ((3, 64, 128), (20, 700, 300), (130, 1056, 256), (270, 2000, 130)):
         rng = np.random.default_rng(K)
@@ -233,6 +242,22 @@ def test_inner_product_of_exact_sums(block):
         y = torch.empty(Bn, O, device="cuda")
         B.adaption_fp4_ip_fwd(Bn, K, O, ops[0][0], ops[1][0], None, False, y, B.new_stats())
         assert np.array_equal(y.double().cpu().numpy(), ms.inner_product(ops[0][1], ops[1][1]))
+
+
+@pytest.mark.parametrize("block", [16, 32])
+def test_inner_product_of_more_tiles_than_the_gpu_has_pairs(block):
+    """85 tiles of 256 x 256: some pairs of CTAs work on a second one, in the other accumulator; every dtype."""
+    Bn, O = 1100, 4100
+    for K, dtype in ((300, "f32"), (1300, "bf16"), (64, "f16"), (2900, "f32")):
+        rng = np.random.default_rng(K)
+        x, xv = operand(rng, Bn, K, block, -1 if block == 16 else 0)
+        w, wv = operand(rng, O, K, block)
+        bias = rng.standard_normal(O).astype(np.float32)
+        y, st = torch.empty(Bn, O, dtype=DT[dtype], device="cuda"), B.new_stats()
+        B.adaption_fp4_ip_fwd(Bn, K, O, x, w, dev(bias), True, y, st)
+        check_product(y, xv, wv, bias, True, block, dtype)
+        s = B.read_stats(st)
+        assert s.status == 0 and s.zeros == int((y == 0).sum())
 
 
 @pytest.mark.parametrize("block", [16, 32])
@@ -263,8 +288,10 @@ def test_product_of_real_activations(block):
         assert s.status == 0 and s.zeros == 2 * int((y == 0).sum())
 
 
-def test_infinite_and_nan_results_stay_in_their_places():
+@pytest.mark.parametrize("kernel", ["cluster", "pair"])
+def test_infinite_and_nan_results_stay_in_their_places(kernel):
     """A NaN scale of one row or one channel reaches that row or channel alone; ReLU keeps NaN; fp16 results beyond its range are infinite."""
+    choose(kernel)
     rng = np.random.default_rng(1)
     code = rng.integers(1, 8, (40, 96)).astype(np.uint8)
     byte = np.full((40, 3), 127, np.uint8)
@@ -390,8 +417,10 @@ def test_refusals_of_the_binding():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("kernel", ["cluster", "pair"])
 @pytest.mark.parametrize("Bn", [4, 300])
-def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(Bn):
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(Bn, kernel):
+    choose(kernel)
     rng = np.random.default_rng(2)
     x, xv = operand(rng, Bn, 2048, 16)
     w, wv = operand(rng, 256, 2048, 16)
@@ -402,6 +431,7 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(Bn):
     torch.cuda.synchronize()
     assert B.read_stats(st).status == B.ERR_TIMEOUT
     B.adaption_debug_set("reset")
+    choose(kernel)
     st = B.new_stats()
     B.adaption_fp4_ip_fwd(Bn, 2048, 256, x, w, None, False, y, st)
     check_product(y, xv, wv, None, False, 16, "f32")
