@@ -311,7 +311,7 @@ ADAPTION_API int adaption_choose_frac_bits_from_acc(int64_t max_abs_acc, int32_t
  *   block 32: step = 2^(b - 127), b the block's scale byte (E8M0; 255 is NaN and never written);
  *             `exp` has to be 0;
  *   block 16: step = e4m3(b) * 2^exp, b a byte of E4M3 without sign (at most 448) and exp one
- *             exponent for the whole tensor, -64 <= exp <= 63 (adaption_fp4_choose_exp).
+ *             exponent for the whole tensor, -63 <= exp <= 63 (adaption_fp4_choose_exp).
  * Storage of a tensor of `outer` rows of `inner` elements:
  *   codes    rows of c_stride / 2 bytes, two elements a byte, the even one in bits 0-3; c_stride >= inner is
  *            a multiple of 32.  Behind the last element a row holds zeros.
@@ -341,8 +341,8 @@ typedef struct adaption_matrix {
 /* Bytes of the scale plane (0 for sizes below 1 or another block length). */
 ADAPTION_API size_t adaption_fp4_scale_bytes(int64_t outer, int64_t inner, int32_t block);
 
-/* Host helper, the counterpart of the decimal point for blocks of 16: the smallest exponent in [-64, 63] with which
- * the scale of a block that holds max_abs fits E4M3 (max_abs <= 6 * 448 * 2^exp); -64 for 0.  max_abs must
+/* Host helper, the counterpart of the decimal point for blocks of 16: the smallest exponent in [-63, 63] with which
+ * the scale of a block that holds max_abs fits E4M3 (max_abs <= 6 * 448 * 2^exp); -63 for 0.  max_abs must
  * not be negative or NaN. */
 ADAPTION_API int adaption_fp4_choose_exp(float max_abs, int32_t* h_exp);
 

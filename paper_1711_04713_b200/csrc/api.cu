@@ -492,7 +492,7 @@ size_t adaption_fp4_scale_bytes(int64_t outer, int64_t inner, int32_t block) {
 
 int adaption_fp4_choose_exp(float max_abs, int32_t* h_exp) {
   if (h_exp == nullptr || !(max_abs >= 0.f)) return ADAPTION_ERR_INVALID_ARG;
-  int e = -64;
+  int e = -63;
   while (e < 63 && (double)max_abs > std::ldexp(2688.0, e)) ++e;
   *h_exp = e;
   return ADAPTION_OK;
@@ -532,7 +532,7 @@ int adaption_fp4_act_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_matrix x, 
   if (rc != ADAPTION_OK || B == 0) return rc;
   rc = check_matrix(x, K);
   if (rc != ADAPTION_OK) return rc;
-  if (w.block == 32 ? x_exp != 0 : (x_exp < -64 || x_exp > 63)) return ADAPTION_ERR_INVALID_ARG;
+  if (w.block == 32 ? x_exp != 0 : (x_exp < -63 || x_exp > 63)) return ADAPTION_ERR_INVALID_ARG;
   if (d_workspace == nullptr || workspace_bytes < adaption_fp4_act_ip_workspace_bytes(B, K, O, w.block))
     return ADAPTION_ERR_WORKSPACE;
   if (!aligned16(d_workspace)) return ADAPTION_ERR_ALIGNMENT;

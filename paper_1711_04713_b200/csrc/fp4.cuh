@@ -95,6 +95,16 @@ __device__ __forceinline__ float e4m3_value(uint32_t byte) {
 __device__ __forceinline__ float e8m0_value(uint32_t byte) {
   return __uint_as_float(byte == 0u ? 0x00400000u : (byte == 255u ? 0x7fc00000u : byte << 23));
 }
+// Two numbers rounded to a 16-bit type, as one word.
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if (DT == ADAPTION_F16) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 // 2^e for e in [-126, 127]
 __host__ __device__ __forceinline__ float pow2_float(int e) {
   const uint32_t b = (uint32_t)(e + 127) << 23;

@@ -45,7 +45,7 @@ struct FpParams {
   uint32_t b_bytes, stage_bytes, tmem_cols, sf_col;
   const uint8_t* sfa;
   const uint8_t* sfb;
-  float unit_x, unit_w;         // 2^exp of the operands
+  float unit;                   // 2^(sum of the operands' exponents)
   const float* bias;
   int relu;
   void* y;
@@ -87,10 +87,13 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
   return v;
 }
 
-// `n` (at most 4) consecutive outputs
-__device__ __forceinline__ void store_outputs(const FpParams& p, long long at, const float (&v)[4], int n) {
+// `n` (at most 4) consecutive outputs; returns how many are stored as 0
+__device__ __forceinline__ uint32_t store_outputs(const FpParams& p, long long at, const float (&v)[4], int n) {
+  uint32_t zeros = 0;
   if (p.dtype == ADAPTION_F32) {
     float* y = reinterpret_cast<float*>(p.y) + at;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) zeros += k < n && v[k] == 0.f;
     if (n == 4 && (reinterpret_cast<uintptr_t>(y) & 15) == 0) {
       *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
     } else {
@@ -98,20 +101,14 @@ __device__ __forceinline__ void store_outputs(const FpParams& p, long long at, c
       for (int k = 0; k < 4; ++k)
         if (k < n) y[k] = v[k];
     }
-    return;
+    return zeros;
   }
   uint32_t w[2];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    if (p.dtype == ADAPTION_F16) {
-      const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-      w[k] = *reinterpret_cast<const uint32_t*>(&h);
-    } else {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-      w[k] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-  }
+  for (int k = 0; k < 2; ++k) w[k] = p.dtype == ADAPTION_F16 ? pack2<ADAPTION_F16>(v[2 * k], v[2 * k + 1]) : pack2<ADAPTION_BF16>(v[2 * k], v[2 * k + 1]);
   uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + at;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) zeros += k < n && ((w[k >> 1] >> (16 * (k & 1))) & 0x7fffu) == 0u;
   if (n == 4 && (reinterpret_cast<uintptr_t>(y) & 7) == 0) {
     *reinterpret_cast<uint2*>(y) = make_uint2(w[0], w[1]);
   } else {
@@ -119,6 +116,7 @@ __device__ __forceinline__ void store_outputs(const FpParams& p, long long at, c
     for (int k = 0; k < 4; ++k)
       if (k < n) y[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
   }
+  return zeros;
 }
 
 // One cluster of S CTAs per tile of 128 channels x BN batch rows: each CTA reduces its share of the k-blocks, leaves
@@ -282,12 +280,10 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       const int o = o0 + 4 * lane, n = min(4, p.O - o);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        v[k] = v[k] * p.unit_x * p.unit_w;
-        if (p.bias != nullptr && k < n) v[k] += p.bias[o + k];
+        v[k] = fmaf(v[k], p.unit, p.bias != nullptr && k < n ? __ldg(p.bias + o + k) : 0.f);
         if (p.relu) v[k] = v[k] < 0.f ? 0.f : v[k];
-        zeros += k < n && v[k] == 0.f;
       }
-      if (n > 0) store_outputs(p, (long long)(b0 + c) * p.y_stride + o, v, n);
+      if (n > 0) zeros += store_outputs(p, (long long)(b0 + c) * p.y_stride + o, v, n);
     }
   }
   __syncwarp();
@@ -378,8 +374,7 @@ static int launch_fp4_cluster(const Fp4Problem& g) {
   smem += 1024;
   p.sfa = (const uint8_t*)g.w.scales;
   p.sfb = (const uint8_t*)g.x.scales;
-  p.unit_x = pow2_float(g.x.exp);
-  p.unit_w = pow2_float(g.w.exp);
+  p.unit = pow2_float(g.x.exp + g.w.exp);
   p.bias = g.bias;
   p.relu = g.relu ? 1 : 0;
   p.y = g.y.data;

@@ -73,12 +73,5 @@ __device__ __forceinline__ uint32_t make_idesc_fp4(int block, int n, int m) {
 __device__ __forceinline__ uint32_t scale_half(uint32_t half) { return (half * 2u) << 4 | (half * 2u) << 29; }
 
 
-template <int DT>
-__device__ __forceinline__ void store_output(void* y, long long at, float v) {
-  if (DT == ADAPTION_F32) reinterpret_cast<float*>(y)[at] = v;
-  else if (DT == ADAPTION_F16) reinterpret_cast<__half*>(y)[at] = __float2half_rn(v);
-  else reinterpret_cast<__nv_bfloat16*>(y)[at] = __float2bfloat16_rn(v);
-}
-
 }  // namespace
 }  // namespace adaption

@@ -31,6 +31,7 @@ constexpr int kMaxStages = 6;
 constexpr int kThreads = 384;              // warp 0: copies; 1: MMA (leader); 4-11: epilogue
 constexpr int kFirstEpiWarp = 4, kEpiWarps = 8;
 constexpr uint32_t kTmemCols = 512;
+constexpr size_t kSmemLimit = 225 * 1024;  // of 227 KB, less barriers and biases
 
 // shared columns of the two accumulators = columns of the scales of two k-blocks
 __host__ __device__ constexpr int scale_columns(int block) { return groups_of(block) * 4 * 3; }
@@ -40,14 +41,15 @@ __host__ __device__ constexpr uint32_t stage_bytes(int block) { return 2 * kAByt
 
 struct PairParams {
   int O, B;
-  int tiles_o, tiles;
+  int tiles_a, tiles;           // tiles along A; all
   int num_kb, steps_last, groups_last;
   int stages;
-  float unit_x, unit_w;
+  float unit;                   // 2^(sum of the operands' exponents)
   const float* bias;
   int relu;
-  void* y;
-  long long y_stride;
+  uint8_t* y;
+  long long y_pitch;            // bytes
+  int aligned32;                // rows of y lie on 32-byte boundaries
   adaption_stats* stats;
   unsigned long long timeout_ns;
   int stall_at;
@@ -80,40 +82,187 @@ __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, PairCtr
   return pair_wait_slow(bar, parity, ctrl, p);
 }
 
-// 8 * N consecutive columns
+// 16 * N consecutive columns of the accumulator
 template <int N>
-__device__ __forceinline__ void load_columns(uint32_t taddr, int32_t (&r)[N][8]) {
+__device__ __forceinline__ void load_columns(uint32_t taddr, int32_t (&r)[2 * N][8]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) tmem_ld8(taddr + 8u * i, r[i]);
+  for (int i = 0; i < N; ++i) tmem_ld16(taddr + 16u * i, r[2 * i], r[2 * i + 1]);
   tmem_ld_wait();
 #pragma unroll
-  for (int i = 0; i < N; ++i) pin_after_wait(r[i]);
-}
-// ... finished and stored: column j is batch row b + j, this lane is channel o
-template <int DT, int N>
-__device__ __forceinline__ void store_columns(const PairParams& p, const int32_t (&r)[N][8], int b, int o, float bias,
-                                              uint32_t& zeros) {
-  if (o >= p.O) return;
-  const int n = min(8 * N, p.B - b);
-  long long at = (long long)b * p.y_stride + o;
-#pragma unroll
-  for (int j = 0; j < 8 * N; ++j) {
-    if (j >= n) break;
-    float v = fmaf(__int_as_float(r[j >> 3][j & 7]) * p.unit_x, p.unit_w, bias);
-    if (p.relu) v = v < 0.f ? 0.f : v;
-    zeros += v == 0.f;
-    store_output<DT>(p.y, at, v);
-    at += p.y_stride;
-  }
-}
-template <int DT, int N>
-__device__ __forceinline__ void finish_columns(const PairParams& p, uint32_t taddr, int b, int o, float bias, uint32_t& zeros) {
-  int32_t r[N][8];
-  load_columns<N>(taddr, r);
-  store_columns<DT, N>(p, r, b, o, bias, zeros);
+  for (int i = 0; i < 2 * N; ++i) pin_after_wait(r[i]);
 }
 
-template <int BLOCK, int DT>
+// Outputs stored as 0 of one lane and tile: pairs of 16-bit outputs are compared and counted together, in their own type (a
+// lane has at most 128 of them, all counts are exact).
+template <int DT>
+struct ZeroCount {
+  uint32_t n = 0;
+  __half2 h = __floats2half2_rn(0.f, 0.f);
+  __nv_bfloat162 b = __floats2bfloat162_rn(0.f, 0.f);
+  __device__ __forceinline__ void pair(uint32_t w) {
+    if (DT == ADAPTION_F16) h = __hadd2(h, __heq2(*reinterpret_cast<__half2*>(&w), __floats2half2_rn(0.f, 0.f)));
+    else b = __hadd2(b, __heq2(*reinterpret_cast<__nv_bfloat162*>(&w), __floats2bfloat162_rn(0.f, 0.f)));
+  }
+  __device__ __forceinline__ uint32_t total() const {
+    if (DT == ADAPTION_F32) return n;
+    const float2 f = DT == ADAPTION_F16 ? __half22float2(h) : __bfloat1622float2(b);
+    return n + (uint32_t)(f.x + f.y);
+  }
+};
+template <int DT>
+__device__ __forceinline__ uint32_t relu2(uint32_t w) {       // (a NaN stays one)
+  if (DT == ADAPTION_F16) {
+    const __half2 m = __hmax2_nan(*reinterpret_cast<__half2*>(&w), __floats2half2_rn(0.f, 0.f));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  }
+  const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&w), __floats2bfloat162_rn(0.f, 0.f));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+__device__ __forceinline__ float relu1(float v) {
+  asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v));
+  return v;
+}
+
+// Lanes are batch rows, columns are channels: 16 of them from channel `c` on become one or two 32-byte pieces of this lane's row.
+template <int DT>
+__device__ __forceinline__ void finish_row(const PairParams& p, const int32_t* r, uint8_t* row, int c, const float* bias,
+                                           ZeroCount<DT>& zeros) {
+  const int n = p.O - c;                               // channels that exist
+  float v[16];
+#pragma unroll
+  for (int j = 0; j < 16; j += 4) {
+    const float4 b = *reinterpret_cast<const float4*>(bias + j);
+    v[j] = fmaf(__int_as_float(r[j]), p.unit, b.x);
+    v[j + 1] = fmaf(__int_as_float(r[j + 1]), p.unit, b.y);
+    v[j + 2] = fmaf(__int_as_float(r[j + 2]), p.unit, b.z);
+    v[j + 3] = fmaf(__int_as_float(r[j + 3]), p.unit, b.w);
+  }
+  if constexpr (DT == ADAPTION_F32) {
+    if (p.relu) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = relu1(v[j]);
+    }
+    float* const y = reinterpret_cast<float*>(row) + c;
+    if (n >= 16) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) zeros.n += v[j] == 0.f;
+#pragma unroll
+      for (int j = 0; j < 16; j += 4) reinterpret_cast<float4*>(y)[j / 4] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if (j >= n) break;
+        zeros.n += v[j] == 0.f;
+        y[j] = v[j];
+      }
+    }
+    return;
+  }
+  uint32_t w[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+  if (p.relu) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = relu2<DT>(w[j]);
+  }
+  uint16_t* const y = reinterpret_cast<uint16_t*>(row) + c;
+  if (n >= 16) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) zeros.pair(w[j]);
+    if (p.aligned32) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(y), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                   "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                   : "memory");
+    } else {
+      reinterpret_cast<uint4*>(y)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      reinterpret_cast<uint4*>(y)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (j >= n) break;
+      const uint16_t h = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+      zeros.n += (h & 0x7fffu) == 0u;
+      y[j] = h;
+    }
+  }
+}
+
+// Lanes are channels, columns are batch rows: 16 rows from `row` on, this lane's channel of each (consecutive lanes store
+// consecutive outputs, so rows of any alignment do).
+template <int DT>
+__device__ __forceinline__ void finish_channel(const PairParams& p, const int32_t* r, uint8_t* at, int rows, float bias,
+                                               ZeroCount<DT>& zeros) {
+#pragma unroll
+  for (int j = 0; j < 16; j += 2) {
+    if (j >= rows) break;
+    float a = fmaf(__int_as_float(r[j]), p.unit, bias), b = fmaf(__int_as_float(r[j + 1]), p.unit, bias);
+    uint8_t* const next = at + p.y_pitch;
+    if (DT == ADAPTION_F32) {
+      if (p.relu) { a = relu1(a); b = relu1(b); }
+      zeros.n += a == 0.f;
+      *reinterpret_cast<float*>(at) = a;
+      if (j + 1 < rows) {
+        zeros.n += b == 0.f;
+        *reinterpret_cast<float*>(next) = b;
+      }
+    } else {
+      uint32_t w = pack2<DT>(a, b);
+      if (p.relu) w = relu2<DT>(w);
+      *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
+      if (j + 1 < rows) {
+        zeros.pair(w);
+        *reinterpret_cast<uint16_t*>(next) = (uint16_t)(w >> 16);
+      } else {
+        zeros.n += (w & 0x7fffu) == 0u;
+      }
+    }
+    at = next + p.y_pitch;
+  }
+}
+
+// What a lane of the epilogue knows about its tile.
+struct TileLane {
+  uint8_t* y;          // ROWS: start of this lane's row; else this lane's channel in the tile's first row
+  int first;           // first channel (ROWS) or batch row of the tile
+  float bias;          // of this lane's channel
+  const float* biases; // ROWS: of the tile's channels
+  bool real;           // the lane's row or channel exists
+};
+template <int DT, bool ROWS, int N>
+__device__ __forceinline__ void finish_columns(const PairParams& p, const int32_t (&r)[2 * N][8], const TileLane& t, int c,
+                                               ZeroCount<DT>& zeros) {
+  if (!t.real) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int at = c + 16 * i;
+    if (ROWS)
+      finish_row<DT>(p, &r[2 * i][0], t.y, t.first + at, t.biases + at, zeros);
+    else
+      finish_channel<DT>(p, &r[2 * i][0], t.y + (long long)at * p.y_pitch, p.B - t.first - at, t.bias, zeros);
+  }
+}
+template <int DT, bool ROWS, int N>
+__device__ __forceinline__ void finish_rest(const PairParams& p, uint32_t acc, const TileLane& t, int c, ZeroCount<DT>& zeros) {
+  int32_t r[2 * N][8];
+  load_columns<N>(acc + (uint32_t)c, r);
+  finish_columns<DT, ROWS, N>(p, r, t, c, zeros);
+}
+// The shared columns: handed back as soon as they are in registers.
+template <int DT, bool ROWS, int N>
+__device__ __forceinline__ void finish_shared(const PairParams& p, uint32_t acc, const TileLane& t, int c, PairCtrl* ctrl, int lane,
+                                              ZeroCount<DT>& zeros) {
+  int32_t r[2 * N][8];
+  load_columns<N>(acc + (uint32_t)c, r);
+  tc_fence_before();
+  __syncwarp();
+  if (lane == 0) mbar_arrive_cluster(mapa_rank(smem_u32(&ctrl->acc_free), 0));
+  finish_columns<DT, ROWS, N>(p, r, t, c, zeros);
+}
+
+// ROWS: the 128-row operand A is the batch (lanes of the accumulators are batch rows) and the columns are channels; otherwise
+// A is the weights.  map_a, map_sfa and so on are of the operand in that place.
+template <int BLOCK, int DT, bool ROWS>
 __global__ void __launch_bounds__(kThreads, 1)
 fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb, const PairParams p) {
@@ -124,6 +273,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   constexpr uint32_t kStage = stage_bytes(BLOCK);
   extern __shared__ uint8_t smem_raw[];
   __shared__ PairCtrl ctrl;
+  __shared__ __align__(16) float bias_tile[ROWS ? kTile : 4];
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
@@ -157,11 +307,11 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 
   bool ok = true;
   if (warp == 0) {
-    // ---- copies: this CTA's 128 channels and its half of the batch rows, their scales; reported to the leader's barrier
+    // ---- copies: this CTA's 128 rows of A, its half of the rows of B, the scales of both; reported to the leader's barrier
     uint32_t it = 0, ph = 0;
     int s = 0;
     for (int t = worker; ok && t < p.tiles; t += workers) {
-      const int to = t % p.tiles_o, tb = t / p.tiles_o;
+      const int ta = t % p.tiles_a, tb = t / p.tiles_a;
       for (int kb = 0; kb < p.num_kb; ++kb) {
         if ((int)it == p.stall_at) { ok = false; break; }
         ok = __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.empty[s]), ph ^ 1u, &ctrl, p));
@@ -171,9 +321,9 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
           if (rank == 0) mbar_expect_tx(own, 2u * kStage);
           const uint32_t full = mapa_rank(own, 0);
           const int words = kb * kGroups * (kFp4TileBytes / 8);
-          tma_load_2d<true>(dst, &map_a, full, kb * kBlockBytes, to * kTile + (int)rank * kRows);
+          tma_load_2d<true>(dst, &map_a, full, kb * kBlockBytes, ta * kTile + (int)rank * kRows);
           tma_load_2d<true>(dst + kABytes, &map_b, full, kb * kBlockBytes, tb * kTile + (int)rank * kRows);
-          tma_load_2d<true>(dst + 2 * kABytes, &map_sfa, full, words, to * 2 + (int)rank);
+          tma_load_2d<true>(dst + 2 * kABytes, &map_sfa, full, words, ta * 2 + (int)rank);
           tma_load_2d<true>(dst + 2 * kABytes + sf_bytes(BLOCK), &map_sfb, full, words, tb * 2);
         }
         __syncwarp();
@@ -258,41 +408,60 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     // ---- epilogue: two warps per lane quarter, each half of the columns
     const int quarter = warp & 3, half = (warp - kFirstEpiWarp) >> 2;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-    uint32_t zeros = 0;
+    uint32_t counted = 0;
     int local = 0;
     for (int t = worker; t < p.tiles; t += workers, ++local) {
-      const int o = (t % p.tiles_o) * kTile + (int)rank * kRows + quarter * 32 + lane, b0 = (t / p.tiles_o) * kTile;
-      const float bias = p.bias != nullptr && o < p.O ? __ldg(p.bias + o) : 0.f;
-      ok = __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.acc_full[local & 1]), (uint32_t)(local >> 1) & 1u, &ctrl, p));
-      if (!ok) break;
+      const int ta = t % p.tiles_a, tb = t / p.tiles_a;
+      const int at = ta * kTile + (int)rank * kRows + quarter * 32 + lane;          // this lane's row of A
+      TileLane tile;
+      tile.first = tb * kTile;
+      tile.real = at < (ROWS ? p.B : p.O);
+      tile.bias = 0.f;
+      tile.biases = bias_tile;
+      if (ROWS) {
+        tile.y = p.y + (long long)at * p.y_pitch;
+        // the channels' biases; every warp has left the last tile's behind when all come here
+        const int i = (int)threadIdx.x - 32 * kFirstEpiWarp, o = tile.first + i;
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
+        bias_tile[i] = p.bias != nullptr && o < p.O ? __ldg(p.bias + o) : 0.f;
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
+      } else {
+        tile.y = p.y + (long long)tile.first * p.y_pitch + (long long)at * (DT == ADAPTION_F32 ? 4 : 2);
+        if (p.bias != nullptr && tile.real) tile.bias = __ldg(p.bias + at);
+      }
+      // (a wait that ran out in one warp is seen by the others at their next one)
+      ok = ok && __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.acc_full[local & 1]), (uint32_t)(local >> 1) & 1u, &ctrl, p));
+      if (!ok) {
+        if (ROWS) continue;              // (the others still meet at the barriers)
+        break;
+      }
       tc_fence_after();
+      ZeroCount<DT> zeros;
       // the columns that the next tile's accumulator shares first: the last ones of the first accumulator, the first ones
-      // of the second
-      constexpr int kMine = kShared / 2, kRest = (kTile - kShared) / 2;          // 24 or 48; 104 or 80
+      // of the second; in runs of 16
       const uint32_t acc = lanes + ((local & 1) ? kSecond : 0u);
       const int first = (local & 1) ? 0 : (int)kSecond, rest = (local & 1) ? kShared : 0;
-      {
-        int32_t r[kMine / 8][8];
-        const int c = first + half * kMine;
-        load_columns<kMine / 8>(acc + (uint32_t)c, r);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(mapa_rank(smem_u32(&ctrl.acc_free), 0));
-        store_columns<DT, kMine / 8>(p, r, b0 + c, o, bias, zeros);
-      }
-      int c = rest + half * kRest;
       if (BLOCK == 32) {
-        finish_columns<DT, 5>(p, acc + (uint32_t)c, b0 + c, o, bias, zeros);
-        finish_columns<DT, 4>(p, acc + (uint32_t)(c + 40), b0 + c + 40, o, bias, zeros);
-        finish_columns<DT, 4>(p, acc + (uint32_t)(c + 72), b0 + c + 72, o, bias, zeros);
+        if (half == 0) {
+          finish_shared<DT, ROWS, 2>(p, acc, tile, first, &ctrl, lane, zeros);
+          finish_rest<DT, ROWS, 3>(p, acc, tile, rest, zeros);
+          finish_rest<DT, ROWS, 3>(p, acc, tile, rest + 48, zeros);
+        } else {
+          finish_shared<DT, ROWS, 1>(p, acc, tile, first + 32, &ctrl, lane, zeros);
+          finish_rest<DT, ROWS, 3>(p, acc, tile, rest + 96, zeros);
+          finish_rest<DT, ROWS, 2>(p, acc, tile, rest + 144, zeros);
+          finish_rest<DT, ROWS, 2>(p, acc, tile, rest + 176, zeros);
+        }
       } else {
-        finish_columns<DT, 5>(p, acc + (uint32_t)c, b0 + c, o, bias, zeros);
-        finish_columns<DT, 5>(p, acc + (uint32_t)(c + 40), b0 + c + 40, o, bias, zeros);
+        finish_shared<DT, ROWS, 3>(p, acc, tile, first + 48 * half, &ctrl, lane, zeros);
+        finish_rest<DT, ROWS, 3>(p, acc, tile, rest + 80 * half, zeros);
+        finish_rest<DT, ROWS, 2>(p, acc, tile, rest + 80 * half + 48, zeros);
       }
+      counted += zeros.total();
     }
     __syncwarp();
-    zeros = __reduce_add_sync(0xffffffffu, zeros);
-    if (lane == 0 && zeros) atomicAdd((unsigned long long*)&p.stats->zeros, (unsigned long long)zeros);
+    counted = __reduce_add_sync(0xffffffffu, counted);
+    if (lane == 0 && counted) atomicAdd((unsigned long long*)&p.stats->zeros, (unsigned long long)counted);
   }
 
   tc_fence_before();
@@ -304,7 +473,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   }
 }
 
-template <int BLOCK, int DT>
+template <int BLOCK, int DT, bool ROWS>
 int launch_pair(const CUtensorMap* maps, const PairParams& p, int grid, cudaStream_t stream) {
   const size_t smem = (size_t)p.stages * stage_bytes(BLOCK) + 1024;
   static std::atomic<uint64_t> prepared{0};
@@ -312,8 +481,8 @@ int launch_pair(const CUtensorMap* maps, const PairParams& p, int grid, cudaStre
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_failure(e, "fp4_pair_kernel device");
   if (dev >= 64 || !((prepared.load(std::memory_order_acquire) >> dev) & 1)) {
-    e = cudaFuncSetAttribute(fp4_pair_kernel<BLOCK, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)(kMaxStages * stage_bytes(BLOCK) + 1024 < 226 * 1024 ? kMaxStages * stage_bytes(BLOCK) + 1024 : 226 * 1024));
+    e = cudaFuncSetAttribute(fp4_pair_kernel<BLOCK, DT, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)kSmemLimit);
     if (e != cudaSuccess) return cuda_failure(e, "fp4_pair_kernel attribute");
     if (dev < 64) prepared.fetch_or((uint64_t)1 << dev, std::memory_order_release);
   }
@@ -331,7 +500,7 @@ int launch_pair(const CUtensorMap* maps, const PairParams& p, int grid, cudaStre
   cfg.attrs = attr;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
   count_launch();
-  e = cudaLaunchKernelEx(&cfg, fp4_pair_kernel<BLOCK, DT>, maps[0], maps[1], maps[2], maps[3], p);
+  e = cudaLaunchKernelEx(&cfg, fp4_pair_kernel<BLOCK, DT, ROWS>, maps[0], maps[1], maps[2], maps[3], p);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return cuda_failure(e, "fp4_pair_kernel launch");
@@ -339,11 +508,11 @@ int launch_pair(const CUtensorMap* maps, const PairParams& p, int grid, cudaStre
   return ADAPTION_OK;
 }
 
-template <int BLOCK>
+template <int BLOCK, bool ROWS>
 int launch_pair(const CUtensorMap* maps, const PairParams& p, int dtype, int grid, cudaStream_t stream) {
-  if (dtype == ADAPTION_F32) return launch_pair<BLOCK, ADAPTION_F32>(maps, p, grid, stream);
-  if (dtype == ADAPTION_F16) return launch_pair<BLOCK, ADAPTION_F16>(maps, p, grid, stream);
-  return launch_pair<BLOCK, ADAPTION_BF16>(maps, p, grid, stream);
+  if (dtype == ADAPTION_F32) return launch_pair<BLOCK, ADAPTION_F32, ROWS>(maps, p, grid, stream);
+  if (dtype == ADAPTION_F16) return launch_pair<BLOCK, ADAPTION_F16, ROWS>(maps, p, grid, stream);
+  return launch_pair<BLOCK, ADAPTION_BF16, ROWS>(maps, p, grid, stream);
 }
 
 }  // namespace
@@ -361,8 +530,15 @@ int launch_fp4_pair(const Fp4Problem& g) {
   std::memset(&p, 0, sizeof(p));
   p.O = (int)g.O;
   p.B = (int)g.B;
-  p.tiles_o = (p.O + kTile - 1) / kTile;
-  const int64_t tiles = (int64_t)p.tiles_o * ((p.B + kTile - 1) / kTile);
+  const int size = dtype_size(g.y.dtype);
+  p.y = (uint8_t*)g.y.data;
+  p.y_pitch = g.y.stride * size;
+  const bool rows = aligned16(g.y.data) && (p.y_pitch & 15) == 0;
+  p.aligned32 = ((reinterpret_cast<uintptr_t>(g.y.data) | (uintptr_t)p.y_pitch) & 31u) == 0;
+  const adaption_fp4tensor &ta = rows ? g.x : g.w, &tb = rows ? g.w : g.x;
+  const int na = rows ? p.B : p.O, nb = rows ? p.O : p.B;
+  p.tiles_a = (na + kTile - 1) / kTile;
+  const int64_t tiles = (int64_t)p.tiles_a * ((nb + kTile - 1) / kTile);
   if (tiles > 0x3fffffff) return ADAPTION_ERR_UNSUPPORTED;
   p.tiles = (int)tiles;
   p.num_kb = (int)((g.K + kBlockElems - 1) / kBlockElems);
@@ -370,35 +546,34 @@ int launch_fp4_pair(const Fp4Problem& g) {
   const int k_last = (int)(g.K - (int64_t)(p.num_kb - 1) * kBlockElems);
   p.steps_last = (k_last + kStepElems - 1) / kStepElems;
   p.groups_last = (int)(groups - (int64_t)(p.num_kb - 1) * groups_of(block));
-  p.stages = (int)((226 * 1024 - 1024) / stage_bytes(block));
+  p.stages = (int)((kSmemLimit - 1024) / stage_bytes(block));
   if (p.stages > kMaxStages) p.stages = kMaxStages;
-  p.unit_x = pow2_float(g.x.exp);
-  p.unit_w = pow2_float(g.w.exp);
+  p.unit = pow2_float(g.x.exp + g.w.exp);
   p.bias = g.bias;
   p.relu = g.relu ? 1 : 0;
-  p.y = g.y.data;
-  p.y_stride = g.y.stride;
   p.stats = g.stats;
   p.timeout_ns = wait_limit_ns();
   p.stall_at = knob(kStallAt);
   if (!load_tensor_map_encoders()) return ADAPTION_ERR_CUDA;
   CUtensorMap maps[4];
   const uint64_t bytes = (uint64_t)(g.K + 1) / 2;
-  bool ok = encode_tiled_2d(&maps[0], g.w.codes, bytes, (uint64_t)p.O, (uint64_t)g.w.c_stride / 2, kBlockBytes, kRows,
+  bool ok = encode_tiled_2d(&maps[0], ta.codes, bytes, (uint64_t)na, (uint64_t)ta.c_stride / 2, kBlockBytes, kRows,
                             CU_TENSOR_MAP_SWIZZLE_128B) &&
-            encode_tiled_2d(&maps[1], g.x.codes, bytes, (uint64_t)p.B, (uint64_t)g.x.c_stride / 2, kBlockBytes, kRows,
+            encode_tiled_2d(&maps[1], tb.codes, bytes, (uint64_t)nb, (uint64_t)tb.c_stride / 2, kBlockBytes, kRows,
                             CU_TENSOR_MAP_SWIZZLE_128B);
   // scale planes: one row per row of tiles, in words of 8 bytes; what lies behind the last tile arrives as zeros
   for (int i = 0; ok && i < 2; ++i) {
-    const uint64_t dims[2] = {(uint64_t)groups * (kFp4TileBytes / 8), (uint64_t)(((i ? p.B : p.O) + kRows - 1) / kRows)};
+    const uint64_t dims[2] = {(uint64_t)groups * (kFp4TileBytes / 8), (uint64_t)(((i ? nb : na) + kRows - 1) / kRows)};
     const uint64_t strides[1] = {(uint64_t)groups * kFp4TileBytes};
     const uint32_t box[2] = {(uint32_t)(groups_of(block) * (kFp4TileBytes / 8)), i ? 2u : 1u};
-    ok = encode_tiled_words(&maps[2 + i], i ? g.x.scales : g.w.scales, 2, dims, strides, box);
+    ok = encode_tiled_words(&maps[2 + i], i ? tb.scales : ta.scales, 2, dims, strides, box);
   }
   if (!ok) return ADAPTION_ERR_CUDA;
   int pairs = num_sms() / 2;
   if (pairs > p.tiles) pairs = p.tiles;
-  return block == 32 ? launch_pair<32>(maps, p, g.y.dtype, 2 * pairs, g.stream) : launch_pair<16>(maps, p, g.y.dtype, 2 * pairs, g.stream);
+  if (block == 32)
+    return rows ? launch_pair<32, true>(maps, p, g.y.dtype, 2 * pairs, g.stream) : launch_pair<32, false>(maps, p, g.y.dtype, 2 * pairs, g.stream);
+  return rows ? launch_pair<16, true>(maps, p, g.y.dtype, 2 * pairs, g.stream) : launch_pair<16, false>(maps, p, g.y.dtype, 2 * pairs, g.stream);
 }
 
 }  // namespace adaption

@@ -20,7 +20,7 @@ namespace adaption {
 
 int check_fp4(const adaption_fp4tensor& t, int64_t inner) {
   if (t.block != 16 && t.block != 32) return ADAPTION_ERR_INVALID_ARG;
-  if (t.block == 32 ? t.exp != 0 : (t.exp < -64 || t.exp > 63)) return ADAPTION_ERR_INVALID_ARG;
+  if (t.block == 32 ? t.exp != 0 : (t.exp < -63 || t.exp > 63)) return ADAPTION_ERR_INVALID_ARG;
   if (t.codes == nullptr || t.scales == nullptr) return ADAPTION_ERR_INVALID_ARG;
   if (t.c_stride < inner || (t.c_stride & 31) != 0) return ADAPTION_ERR_INVALID_ARG;
   if (!aligned16(t.codes) || !aligned16(t.scales)) return ADAPTION_ERR_ALIGNMENT;
@@ -331,16 +331,6 @@ struct ValueParams {
   int64_t pitch;                // of a row of y, in bytes
 };
 
-// two values as one word of a 16-bit type
-template <int DT>
-__device__ __forceinline__ uint32_t pack_values(float a, float b) {
-  if (DT == kF16) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 template <int BLOCK>
 __device__ __forceinline__ float step_of(const ValueParams& p, uint32_t byte) {
   return BLOCK == 32 ? e8m0_value(byte) : e4m3_value(byte) * p.unit;
@@ -384,7 +374,7 @@ __global__ void __launch_bounds__(kThreads) fp4_values_kernel(const ValueParams 
         w[2 * k & 7] = __float_as_uint(f.x * s);
         w[(2 * k + 1) & 7] = __float_as_uint(f.y * s);
       } else {
-        w[k] = pack_values<DT>(f.x * s, f.y * s);
+        w[k] = pack2<DT>(f.x * s, f.y * s);
       }
     }
     uint8_t* to = p.y + (int64_t)row[u] * p.pitch + (int64_t)col[u] * (DT == kF32 ? 4 : 2);
@@ -456,7 +446,7 @@ __global__ void __launch_bounds__(kThreads) fp4_values_shifted_kernel(const Valu
           w[e & 7] = __float_as_uint(a);
           w[(e + 1) & 7] = __float_as_uint(b);
         } else {
-          w[e >> 1] = pack_values<DT>(a, b);
+          w[e >> 1] = pack2<DT>(a, b);
         }
       }
     }

@@ -104,7 +104,7 @@ def test_quantize_special_values(block):
     rows = [vals + [0.0] * 16, [0.0] * 32, [np.nan] * 32, [np.inf] * 32, [1e-45] * 32, vals[3:8] + [0.0] * 27,
             [m * s for s in (1.0, 1.875) for m in (0.25, .75, 1.25, 1.75, 2.5, 3.5, 5, 6, -0.25, -.75, -1.25, -1.75, -2.5, -3.5, -5, -6)]]
     x = np.array(rows, np.float32)
-    for exp in ((0,) if block == 32 else (0, -64, 63, -9)):
+    for exp in ((0,) if block == 32 else (0, -63, 63, -9)):
         for relu in (False, True):
             q = B.Fp4Tensor.empty(*x.shape, block, exp)
             B.adaption_fp4_quantize(dev(x), *x.shape, q, relu)
@@ -246,16 +246,20 @@ def test_inner_product_of_exact_sums(block, kernel):
 
 @pytest.mark.parametrize("block", [16, 32])
 def test_inner_product_of_more_tiles_than_the_gpu_has_pairs(block):
-    """85 tiles of 256 x 256: some pairs of CTAs work on a second one, in the other accumulator; every dtype."""
-    Bn, O = 1100, 4100
-    for K, dtype in ((300, "f32"), (1300, "bf16"), (64, "f16"), (2900, "f32")):
+    """85 tiles of 256 x 256: some pairs of CTAs work on a second one, in the other accumulator; every type, rows of outputs on
+    32-byte and 16-byte boundaries and off them."""
+    Bn = 1100
+    for K, O, pad, dtype in ((300, 4112, 0, "f32"), (1300, 4112, 0, "bf16"), (64, 4104, 0, "f16"), (2900, 4101, 0, "f32"), (520, 4112, 1, "bf16"),
+                             (200, 4110, 2, "f16"), (600, 4100, 4, "bf16")):
         rng = np.random.default_rng(K)
         x, xv = operand(rng, Bn, K, block, -1 if block == 16 else 0)
         w, wv = operand(rng, O, K, block)
         bias = rng.standard_normal(O).astype(np.float32)
-        y, st = torch.empty(Bn, O, dtype=DT[dtype], device="cuda"), B.new_stats()
+        full = torch.full((Bn, O + pad), 7.0, dtype=DT[dtype], device="cuda")
+        y, st = full[:, :O], B.new_stats()
         B.adaption_fp4_ip_fwd(Bn, K, O, x, w, dev(bias), True, y, st)
         check_product(y, xv, wv, bias, True, block, dtype)
+        assert bool((full[:, O:] == 7).all())
         s = B.read_stats(st)
         assert s.status == 0 and s.zeros == int((y == 0).sum())
 
