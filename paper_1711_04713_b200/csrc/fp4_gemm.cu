@@ -200,6 +200,7 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     }
     __syncwarp();
   } else if (warp == 1) {
+    const uint32_t issue = elect_one() ? 1u : 0u;
     const uint32_t id = make_idesc_fp4(BLOCK, p.BN, kRows);
     const uint32_t dhi = smem_desc_hi(8u * kBlockBytes, 2u);          // 128-byte swizzle
     const uint32_t shi = smem_desc_hi(128u, 0u);                       // scale tiles: rows of 16 bytes, groups of 8 rows
@@ -216,20 +217,22 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       const uint32_t a = smem_desc_lo(ring) + (uint32_t)s * (p.stage_bytes >> 4), b = a + (kABytes >> 4);
       const uint32_t sf = ((ring + (uint32_t)s * p.stage_bytes + kABytes + p.b_bytes) >> 4) & 0x3FFFu;
       const uint32_t ta = tmem + p.sf_col + (uint32_t)s * slot, tbx = ta + 4u * kGroups;
-      if (elect_one()) {
-        for (int g = 0; g < groups; ++g) {
-          scales_to_tmem<false>(ta + 4u * g, sf + 32u * g, shi);
-          for (int c = 0; c < p.chunks_b; ++c)
-            scales_to_tmem<false>(tbx + cols_b * g + 4u * c, sf + 32u * (uint32_t)((1 + c) * kGroups + g), shi);
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        if (g < groups) {
+          scales_to_tmem<false>(issue, ta + 4u * g, sf + 32u * g, shi);
+          scales_to_tmem<false>(issue, tbx + cols_b * g, sf + 32u * (uint32_t)(kGroups + g), shi);
+          if (p.chunks_b > 1) scales_to_tmem<false>(issue, tbx + cols_b * g + 4u, sf + 32u * (uint32_t)(2 * kGroups + g), shi);
         }
-        for (int k = 0; k < steps; ++k) {
-          const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
-          mma_fp4<BLOCK, false>(tmem, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g,
-                         tbx + cols_b * g, (kb > kb_begin || k > 0) ? 1u : 0u);
-        }
-        tc_commit<false>(smem_u32(&ctrl.empty[s]));
       }
-      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < kBlockElems / kStepElems; ++k) {
+        const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
+        if (k < steps)
+          mma_fp4<BLOCK, false>(issue, tmem, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g,
+                                tbx + cols_b * g, (kb > kb_begin || k > 0) ? 1u : 0u);
+      }
+      tc_commit_if<false>(issue, smem_u32(&ctrl.empty[s]));
       if (++s == p.stages) { s = 0; ph ^= 1u; }
     }
     if (elect_one()) tc_commit<false>(smem_u32(&ctrl.done));

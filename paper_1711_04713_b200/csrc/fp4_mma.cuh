@@ -15,24 +15,65 @@ constexpr uint32_t kABytes = kRows * kBlockBytes;
 
 __host__ __device__ constexpr int groups_of(int block) { return block == 32 ? 2 : 4; }    // scale tiles of a k-block and 128 rows
 
+// Arrival on a barrier of any CTA of the cluster that orders this CTA's work only (TMEM reads, by the fence before it).
+// With release at cluster scope it waited for the warp's stores to global memory: about 1000 cycles.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+// Whether a phase has completed, without waiting for it (try_wait may suspend the thread for microseconds).
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 // contiguous bytes of global memory -> this CTA's shared memory
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
                "r"(bytes), "r"(bar)
                : "memory");
 }
+// A box from shared memory to global memory, clipped at the tensor's ends; completion by groups of the issuing thread.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y)
+               : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// at most N of the thread's last stores still read their shared memory
+template <int N>
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// The issuing warp stays in uniform control flow and the lane with `issue` != 0 (elect_one, once) executes: operands live in
+// uniform registers that way.  (In a branch of the elected lane, the sixteen instructions of a k-block of blocks of 16 took 700
+// cycles to issue, more than the 512 that they run.)
+//
 // One scale tile (32 rows of 16 bytes) from shared memory to four TMEM columns, repeated in all lane quarters.  PAIR: in both
 // CTAs, each from its own shared memory.
 template <bool PAIR>
-__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t desc_lo, uint32_t desc_hi) {
-#define ADAPTION_SCALES(CG)                                    \
-  asm volatile(                                                \
-      "{\n"                                                    \
-      ".reg .b64 d;\n"                                         \
-      "mov.b64 d, {%1, %2};\n"                                 \
-      "tcgen05.cp.cta_group::" CG ".32x128b.warpx4 [%0], d;\n" \
-      "}\n" ::"r"(taddr),                                      \
-      "r"(desc_lo), "r"(desc_hi)                               \
+__device__ __forceinline__ void scales_to_tmem(uint32_t issue, uint32_t taddr, uint32_t desc_lo, uint32_t desc_hi) {
+#define ADAPTION_SCALES(CG)                                       \
+  asm volatile(                                                   \
+      "{\n"                                                       \
+      ".reg .pred e;\n"                                           \
+      ".reg .b64 d;\n"                                            \
+      "setp.ne.b32 e, %3, 0;\n"                                   \
+      "mov.b64 d, {%1, %2};\n"                                    \
+      "@e tcgen05.cp.cta_group::" CG ".32x128b.warpx4 [%0], d;\n" \
+      "}\n" ::"r"(taddr),                                         \
+      "r"(desc_lo), "r"(desc_hi), "r"(issue)                      \
       : "memory")
   if (PAIR)
     ADAPTION_SCALES("2");
@@ -41,19 +82,20 @@ __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t desc_lo,
 #undef ADAPTION_SCALES
 }
 template <int BLOCK, bool PAIR>
-__device__ __forceinline__ void mma_fp4(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t sfa,
-                                        uint32_t sfb, uint32_t accumulate) {
-#define ADAPTION_MMA_FP4(CG, KIND)                                                                  \
+__device__ __forceinline__ void mma_fp4(uint32_t issue, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc,
+                                        uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+#define ADAPTION_MMA_FP4(CG, KIND)                                                                 \
   asm volatile(                                                                                    \
       "{\n"                                                                                        \
-      ".reg .pred p;\n"                                                                            \
+      ".reg .pred p, e;\n"                                                                         \
       ".reg .b64 da, db;\n"                                                                        \
+      "setp.ne.b32 e, %8, 0;\n"                                                                    \
       "setp.ne.b32 p, %5, 0;\n"                                                                    \
       "mov.b64 da, {%1, %3};\n"                                                                    \
       "mov.b64 db, {%2, %3};\n"                                                                    \
-      "tcgen05.mma.cta_group::" CG "." KIND " [%0], da, db, %4, [%6], [%7], p;\n"                  \
+      "@e tcgen05.mma.cta_group::" CG "." KIND " [%0], da, db, %4, [%6], [%7], p;\n"               \
       "}\n" ::"r"(d),                                                                              \
-      "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)          \
+      "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb), "r"(issue) \
       : "memory")
   if (BLOCK == 32 && PAIR)
     ADAPTION_MMA_FP4("2", "kind::mxf4.block_scale.scale_vec::2X");

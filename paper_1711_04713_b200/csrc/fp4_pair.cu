@@ -6,12 +6,17 @@
 // (and 3 or 6 KB of scales) for 512 cycles of the tensor core, at most 76 bytes a cycle; 128 x 256 tiles of single CTAs
 // need 54 KB.
 //
-// TMEM: an accumulator has 256 columns, two have all 512, and the scales of two k-blocks take 48 (blocks of 32) or 96.  So the second
-// accumulator begins in the last 48 or 96 columns of the first.  The epilogue empties the shared columns of a tile first and hands
-// them back; the next tile's MMAs start then, while it works through the others.
+// TMEM: the accumulator has 256 of the 512 columns, the scales of the k-blocks in the ring have the others, a slot per stage of the
+// ring, so that no scale is overwritten before the MMAs that read it have released the stage.  (With slots for two k-blocks the wait
+// for that, about 1000 cycles from the last MMA to the first one of the k-block after next, held a k-block at 870 cycles
+// instead of 512.)  All sixteen warps of the epilogue load a tile's sums at once, 64 columns each, and hand the accumulator
+// back before they work on them: about 700 cycles from a tile's last MMA to the next one's first.  A second accumulator that shares
+// half or more of the columns with the first saves none of it.
 //
-// Scales are copied to TMEM two k-blocks ahead at most: the issuing warp waits until the MMAs of the k-block before the last
-// have retired (their release of the ring's stage says so) before it overwrites the columns they read.
+// Outputs leave by bulk-tensor stores from shared memory where their rows are aligned, one block of 4 KB after the other with
+// three under way.  The 64 KB of a tile take 3500 cycles of the SM's share of L2's writes in any case; stored by the lanes
+// themselves they held up the issuing warp's barrier tests and MMAs for that long (1100 cycles a k-block), as stores issued
+// all at once they held up the copies.
 #include <cuda.h>
 
 #include <cstring>
@@ -27,39 +32,44 @@ int num_sms();
 namespace {
 
 constexpr int kTile = 256;                 // channels and rows of a pair's tile
-constexpr int kMaxStages = 6;
-constexpr int kThreads = 384;              // warp 0: copies; 1: MMA (leader); 4-11: epilogue
-constexpr int kFirstEpiWarp = 4, kEpiWarps = 8;
+constexpr int kStages = 4;
+constexpr int kThreads = 640;              // warp 0: copies; 1: MMA (leader); 3: stores; 4-19: epilogue
+constexpr int kFirstEpiWarp = 4, kEpiWarps = 16;
 constexpr uint32_t kTmemCols = 512;
-constexpr size_t kSmemLimit = 225 * 1024;  // of 227 KB, less barriers and biases
+constexpr uint32_t kScales = kTile;        // first TMEM column of the scales
+constexpr int kWarpCols = kTile / 4;       // columns of an epilogue warp
+constexpr uint32_t kStagingBytes = 32 * 128;   // of an epilogue warp: 32 rows of 128 bytes
 
-// shared columns of the two accumulators = columns of the scales of two k-blocks
+// TMEM columns of the scales of a k-block
 __host__ __device__ constexpr int scale_columns(int block) { return groups_of(block) * 4 * 3; }
-__host__ __device__ constexpr int shared_columns(int block) { return 2 * scale_columns(block); }
 __host__ __device__ constexpr uint32_t sf_bytes(int block) { return (uint32_t)groups_of(block) * kFp4TileBytes; }
 __host__ __device__ constexpr uint32_t stage_bytes(int block) { return 2 * kABytes + 3 * sf_bytes(block); }
+__host__ __device__ constexpr uint32_t smem_bytes(int block) { return kStages * stage_bytes(block) + kEpiWarps * kStagingBytes + 1024; }
+static_assert(kScales + kStages * scale_columns(16) <= kTmemCols, "a slot of scales for every stage");
+static_assert(smem_bytes(16) <= 225 * 1024, "227 KB, less barriers and biases");
 
 struct PairParams {
   int O, B;
   int tiles_a, tiles;           // tiles along A; all
   int num_kb, steps_last, groups_last;
-  int stages;
   float unit;                   // 2^(sum of the operands' exponents)
   const float* bias;
   int relu;
   uint8_t* y;
   long long y_pitch;            // bytes
-  int aligned32;                // rows of y lie on 32-byte boundaries
+  int cols16;                   // channels before the last 16-byte boundary of a row
   adaption_stats* stats;
   unsigned long long timeout_ns;
   int stall_at;
 };
 
 struct PairCtrl {
-  unsigned long long full[kMaxStages];     // the leader's: bytes of both CTAs
-  unsigned long long empty[kMaxStages];    // in both CTAs
-  unsigned long long acc_full[2];          // in both CTAs: a tile's sums are complete
-  unsigned long long acc_free;             // the leader's: the shared columns of a tile have been read
+  unsigned long long full[kStages];     // the leader's: bytes of both CTAs
+  unsigned long long empty[kStages];    // in both CTAs
+  unsigned long long acc_full;             // in both CTAs: a tile's sums are complete
+  unsigned long long acc_free;             // the leader's: they are in registers
+  unsigned long long staged[kEpiWarps];    // an epilogue warp has filled its staging block
+  unsigned long long stored[kEpiWarps];    // the block has been read by its store
   unsigned long long drain;
   uint32_t tmem_base;
   volatile uint32_t abort;
@@ -82,18 +92,30 @@ __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, PairCtr
   return pair_wait_slow(bar, parity, ctrl, p);
 }
 
-// 16 * N consecutive columns of the accumulator
-template <int N>
-__device__ __forceinline__ void load_columns(uint32_t taddr, int32_t (&r)[2 * N][8]) {
+// Scales to TMEM and MMAs of one k-block: `steps` instructions, `groups` scale tiles per 128 rows.
+template <int BLOCK>
+__device__ __forceinline__ void issue_kblock(uint32_t issue, uint32_t d, uint32_t a, uint32_t b, uint32_t dhi, uint32_t id, uint32_t ta,
+                                             uint32_t tb, uint32_t sf, uint32_t shi, uint32_t more, int steps, int groups) {
+  constexpr int kGroups = groups_of(BLOCK);
 #pragma unroll
-  for (int i = 0; i < N; ++i) tmem_ld16(taddr + 16u * i, r[2 * i], r[2 * i + 1]);
-  tmem_ld_wait();
+  for (int g = 0; g < kGroups; ++g) {
+    if (g < groups) {
+      scales_to_tmem<true>(issue, ta + 4u * g, sf + 32u * g, shi);
+      scales_to_tmem<true>(issue, tb + 8u * g, sf + 32u * (kGroups + g), shi);
+      scales_to_tmem<true>(issue, tb + 8u * g + 4u, sf + 32u * (2 * kGroups + g), shi);
+    }
+  }
 #pragma unroll
-  for (int i = 0; i < 2 * N; ++i) pin_after_wait(r[i]);
+  for (int k = 0; k < kBlockElems / kStepElems; ++k) {
+    const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
+    if (k < steps)
+      mma_fp4<BLOCK, true>(issue, d, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g, tb + 8u * g,
+                           k > 0 ? 1u : more);
+  }
 }
 
 // Outputs stored as 0 of one lane and tile: pairs of 16-bit outputs are compared and counted together, in their own type (a
-// lane has at most 128 of them, all counts are exact).
+// lane has 64 of them, all counts are exact).
 template <int DT>
 struct ZeroCount {
   uint32_t n = 0;
@@ -123,67 +145,60 @@ __device__ __forceinline__ float relu1(float v) {
   return v;
 }
 
-// Lanes are batch rows, columns are channels: 16 of them from channel `c` on become one or two 32-byte pieces of this lane's row.
+// Lanes are batch rows, columns are channels: 32 of them from channel `c` on, as half a row (16-bit types: half 0 or 1) or a
+// whole row of the warp's staging block, in the order of the 128-byte swizzle.  The stores from there end on the row's last 16-byte
+// boundary (a store clips at such boundaries only); outputs behind it go to the row `y` at once.
 template <int DT>
-__device__ __forceinline__ void finish_row(const PairParams& p, const int32_t* r, uint8_t* row, int c, const float* bias,
-                                           ZeroCount<DT>& zeros) {
-  const int n = p.O - c;                               // channels that exist
-  float v[16];
+__device__ __forceinline__ void stage_row(const PairParams& p, const int32_t (&r)[32], uint32_t staging, int half, int lane, int c,
+                                          bool real, uint8_t* y, const float* bias, ZeroCount<DT>& zeros) {
+  const int n = real ? p.O - c : 0;                    // channels that exist (what does not is clipped by the store)
+  const uint32_t row = staging + (uint32_t)lane * 128u, key = (uint32_t)lane & 7u;
 #pragma unroll
-  for (int j = 0; j < 16; j += 4) {
-    const float4 b = *reinterpret_cast<const float4*>(bias + j);
-    v[j] = fmaf(__int_as_float(r[j]), p.unit, b.x);
-    v[j + 1] = fmaf(__int_as_float(r[j + 1]), p.unit, b.y);
-    v[j + 2] = fmaf(__int_as_float(r[j + 2]), p.unit, b.z);
-    v[j + 3] = fmaf(__int_as_float(r[j + 3]), p.unit, b.w);
-  }
-  if constexpr (DT == ADAPTION_F32) {
-    if (p.relu) {
+  for (int i = 0; i < 32; i += 8) {                    // eight channels
+    const float4 b0 = *reinterpret_cast<const float4*>(bias + i), b1 = *reinterpret_cast<const float4*>(bias + i + 4);
+    float v[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
 #pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = relu1(v[j]);
-    }
-    float* const y = reinterpret_cast<float*>(row) + c;
-    if (n >= 16) {
+    for (int j = 0; j < 8; ++j) v[j] = fmaf(__int_as_float(r[i + j]), p.unit, v[j]);
+    if constexpr (DT == ADAPTION_F32) {
+      if (p.relu) {
 #pragma unroll
-      for (int j = 0; j < 16; ++j) zeros.n += v[j] == 0.f;
-#pragma unroll
-      for (int j = 0; j < 16; j += 4) reinterpret_cast<float4*>(y)[j / 4] = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        if (j >= n) break;
-        zeros.n += v[j] == 0.f;
-        y[j] = v[j];
+        for (int j = 0; j < 8; ++j) v[j] = relu1(v[j]);
       }
-    }
-    return;
-  }
-  uint32_t w[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
-  if (p.relu) {
+      for (int j = 0; j < 8; ++j) zeros.n += v[j] == 0.f && i + j < n;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = relu2<DT>(w[j]);
-  }
-  uint16_t* const y = reinterpret_cast<uint16_t*>(row) + c;
-  if (n >= 16) {
+      for (int j = 0; j < 8; j += 4) {
+        st_shared_v4(row + ((((uint32_t)(i + j) >> 2) ^ key) << 4), __float_as_uint(v[j]), __float_as_uint(v[j + 1]),
+                     __float_as_uint(v[j + 2]), __float_as_uint(v[j + 3]));
+        const int tail = n - i - j;
+        if (tail > 0 && tail < 4) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) zeros.pair(w[j]);
-    if (p.aligned32) {
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(y), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-                   "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                   : "memory");
+          for (int e = 0; e < 3; ++e)
+            if (e < tail) reinterpret_cast<float*>(y)[c + i + j + e] = v[j + e];
+        }
+      }
     } else {
-      reinterpret_cast<uint4*>(y)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-      reinterpret_cast<uint4*>(y)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-  } else {
+      uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      if (j >= n) break;
-      const uint16_t h = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
-      zeros.n += (h & 0x7fffu) == 0u;
-      y[j] = h;
+      for (int j = 0; j < 4; ++j) w[j] = pack2<DT>(v[2 * j], v[2 * j + 1]);
+      if (p.relu) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = relu2<DT>(w[j]);
+      }
+      if (n >= 32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) zeros.pair(w[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) zeros.n += i + j < n && ((w[j >> 1] >> (16 * (j & 1))) & 0x7fffu) == 0u;
+      }
+      st_shared_v4(row + (((uint32_t)(4 * half + (i >> 3)) ^ key) << 4), w[0], w[1], w[2], w[3]);
+      const int tail = n - i;
+      if (tail > 0 && tail < 8) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+          if (e < tail) reinterpret_cast<uint16_t*>(y)[c + i + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+      }
     }
   }
 }
@@ -221,55 +236,14 @@ __device__ __forceinline__ void finish_channel(const PairParams& p, const int32_
   }
 }
 
-// What a lane of the epilogue knows about its tile.
-struct TileLane {
-  uint8_t* y;          // ROWS: start of this lane's row; else this lane's channel in the tile's first row
-  int first;           // first channel (ROWS) or batch row of the tile
-  float bias;          // of this lane's channel
-  const float* biases; // ROWS: of the tile's channels
-  bool real;           // the lane's row or channel exists
-};
-template <int DT, bool ROWS, int N>
-__device__ __forceinline__ void finish_columns(const PairParams& p, const int32_t (&r)[2 * N][8], const TileLane& t, int c,
-                                               ZeroCount<DT>& zeros) {
-  if (!t.real) return;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int at = c + 16 * i;
-    if (ROWS)
-      finish_row<DT>(p, &r[2 * i][0], t.y, t.first + at, t.biases + at, zeros);
-    else
-      finish_channel<DT>(p, &r[2 * i][0], t.y + (long long)at * p.y_pitch, p.B - t.first - at, t.bias, zeros);
-  }
-}
-template <int DT, bool ROWS, int N>
-__device__ __forceinline__ void finish_rest(const PairParams& p, uint32_t acc, const TileLane& t, int c, ZeroCount<DT>& zeros) {
-  int32_t r[2 * N][8];
-  load_columns<N>(acc + (uint32_t)c, r);
-  finish_columns<DT, ROWS, N>(p, r, t, c, zeros);
-}
-// The shared columns: handed back as soon as they are in registers.
-template <int DT, bool ROWS, int N>
-__device__ __forceinline__ void finish_shared(const PairParams& p, uint32_t acc, const TileLane& t, int c, PairCtrl* ctrl, int lane,
-                                              ZeroCount<DT>& zeros) {
-  int32_t r[2 * N][8];
-  load_columns<N>(acc + (uint32_t)c, r);
-  tc_fence_before();
-  __syncwarp();
-  if (lane == 0) mbar_arrive_cluster(mapa_rank(smem_u32(&ctrl->acc_free), 0));
-  finish_columns<DT, ROWS, N>(p, r, t, c, zeros);
-}
-
 // ROWS: the 128-row operand A is the batch (lanes of the accumulators are batch rows) and the columns are channels; otherwise
 // A is the weights.  map_a, map_sfa and so on are of the operand in that place.
 template <int BLOCK, int DT, bool ROWS>
 __global__ void __launch_bounds__(kThreads, 1)
 fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb, const PairParams p) {
+                const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb,
+                const __grid_constant__ CUtensorMap map_y, const PairParams p) {
   constexpr int kGroups = groups_of(BLOCK);
-  constexpr int kShared = shared_columns(BLOCK);                 // 48 or 96
-  constexpr uint32_t kSecond = kTile - kShared;                  // first column of the second accumulator
-  constexpr uint32_t kScales = kTmemCols - kShared;              // ... of the scales
   constexpr uint32_t kStage = stage_bytes(BLOCK);
   extern __shared__ uint8_t smem_raw[];
   __shared__ PairCtrl ctrl;
@@ -281,17 +255,21 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
   const int worker = (int)(blockIdx.x >> 1), workers = (int)(gridDim.x >> 1);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < p.stages; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       mbar_init(smem_u32(&ctrl.full[s]), 1);
       mbar_init(smem_u32(&ctrl.empty[s]), 1);
     }
-    mbar_init(smem_u32(&ctrl.acc_full[0]), 1);
-    mbar_init(smem_u32(&ctrl.acc_full[1]), 1);
+    mbar_init(smem_u32(&ctrl.acc_full), 1);
     mbar_init(smem_u32(&ctrl.acc_free), 2 * kEpiWarps);
+    for (int w = 0; w < kEpiWarps; ++w) {
+      mbar_init(smem_u32(&ctrl.staged[w]), 1);
+      mbar_init(smem_u32(&ctrl.stored[w]), 1);
+    }
     mbar_init(smem_u32(&ctrl.drain), 1);
     ctrl.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == 0 && lane < 4) prefetch_map(lane == 0 ? &map_a : (lane == 1 ? &map_b : (lane == 2 ? &map_sfa : &map_sfb)));
   if (warp == 2) {
     tmem_alloc<true>(smem_u32(&ctrl.tmem_base), kTmemCols);
     tmem_relinquish<true>();
@@ -328,73 +306,58 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         }
         __syncwarp();
         ++it;
-        if (++s == p.stages) { s = 0; ph ^= 1u; }
+        if (++s == kStages) { s = 0; ph ^= 1u; }
       }
     }
     if ((!ok || ctrl.abort) && lane == 0) {
       // gave up: let the copies in flight land.  (Their bytes are counted on the leader's barriers, so the follower just waits.)
-      const uint32_t n = it < (uint32_t)p.stages ? it : (uint32_t)p.stages;
+      const uint32_t n = it < kStages ? it : kStages;
       const unsigned long long t0 = global_ns();
       for (uint32_t j = it - n; j < it; ++j) {
         while (global_ns() - t0 < 5000000ull &&
-               (rank != 0 || !mbar_try_wait(smem_u32(&ctrl.full[j % (uint32_t)p.stages]), (j / (uint32_t)p.stages) & 1u))) {
+               (rank != 0 || !mbar_try_wait(smem_u32(&ctrl.full[j % kStages]), (j / kStages) & 1u))) {
         }
       }
     }
     __syncwarp();
   } else if (warp == 1 && rank == 0) {
     // ---- MMA issue
+    const uint32_t issue = elect_one() ? 1u : 0u;
     const uint32_t id = make_idesc_fp4(BLOCK, kTile, kTile);
     const uint32_t dhi = smem_desc_hi(8u * kBlockBytes, 2u);          // 128-byte swizzle
     const uint32_t shi = smem_desc_hi(128u, 0u);                       // scale tiles: rows of 16 bytes, groups of 8 rows
-    uint32_t it = 0, ph = 0, prev_ph = 0;
-    int s = 0, prev = -1, prev2 = -1;                                  // stages of the last two k-blocks
-    uint32_t prev2_ph = 0;
-    int local = 0;
+    uint32_t ph = 0;
+    int s = 0, local = 0;
+    bool full_next = false;
     for (int t = worker; ok && t < p.tiles; t += workers, ++local) {
       if (local > 0) {
         ok = __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.acc_free), (uint32_t)(local - 1) & 1u, &ctrl, p));
         if (!ok) break;
         tc_fence_after();
       }
-      const uint32_t d = tmem + ((local & 1) ? kSecond : 0u);
       for (int kb = 0; kb < p.num_kb; ++kb) {
-        ok = __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.full[s]), ph, &ctrl, p));
-        if (ok && prev2 >= 0)
-          ok = __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.empty[prev2]), prev2_ph, &ctrl, p));
+        // (looked at while the k-block before was issued)
+        if (!full_next) ok = __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.full[s]), ph, &ctrl, p));
         if (!ok) break;
+        const int next_s = s + 1 == kStages ? 0 : s + 1;
+        const uint32_t next_ph = next_s == 0 ? ph ^ 1u : ph;
+        full_next = __all_sync(0xffffffffu, mbar_test(smem_u32(&ctrl.full[next_s]), next_ph));
         tc_fence_after();
         const uint32_t a = smem_desc_lo(ring) + (uint32_t)s * (kStage >> 4), b = a + (kABytes >> 4);
         const uint32_t sf = ((ring + (uint32_t)s * kStage + 2 * kABytes) >> 4) & 0x3FFFu;
-        const uint32_t ta = tmem + kScales + (it & 1u) * (uint32_t)scale_columns(BLOCK), tb = ta + 4u * kGroups;
+        const uint32_t ta = tmem + kScales + (uint32_t)s * (uint32_t)scale_columns(BLOCK), tb = ta + 4u * kGroups;
         const bool last = kb == p.num_kb - 1;
-        const int steps = last ? p.steps_last : kBlockElems / kStepElems, groups = last ? p.groups_last : kGroups;
-        if (elect_one()) {
-#pragma unroll
-          for (int g = 0; g < kGroups; ++g) {
-            if (g < groups) {
-              scales_to_tmem<true>(ta + 4u * g, sf + 32u * g, shi);
-              scales_to_tmem<true>(tb + 8u * g, sf + 32u * (kGroups + g), shi);
-              scales_to_tmem<true>(tb + 8u * g + 4u, sf + 32u * (2 * kGroups + g), shi);
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < kBlockElems / kStepElems; ++k) {
-            const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
-            if (k < steps)
-              mma_fp4<BLOCK, true>(d, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g,
-                                   tb + 8u * g, (kb > 0 || k > 0) ? 1u : 0u);
-          }
-          tc_commit<true>(smem_u32(&ctrl.empty[s]));
+        const uint32_t more = kb > 0 ? 1u : 0u;
+        if (!last) {
+          issue_kblock<BLOCK>(issue, tmem, a, b, dhi, id, ta, tb, sf, shi, more, kBlockElems / kStepElems, kGroups);
+        } else {
+          issue_kblock<BLOCK>(issue, tmem, a, b, dhi, id, ta, tb, sf, shi, more, p.steps_last, p.groups_last);
         }
-        __syncwarp();
-        prev2 = prev; prev2_ph = prev_ph;
-        prev = s; prev_ph = ph;
-        ++it;
-        if (++s == p.stages) { s = 0; ph ^= 1u; }
+        tc_commit_if<true>(issue, smem_u32(&ctrl.empty[s]));
+        s = next_s;
+        ph = next_ph;
       }
-      if (ok && elect_one()) tc_commit<true>(smem_u32(&ctrl.acc_full[local & 1]));
-      __syncwarp();
+      if (ok) tc_commit_if<true>(issue, smem_u32(&ctrl.acc_full));
     }
     if ((!ok || ctrl.abort) && lane == 0) {
       // no MMA may still read shared memory or write TMEM when the CTAs tear down
@@ -404,58 +367,92 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
       }
     }
     __syncwarp();
+  } else if (warp == 3 && ROWS) {
+    // ---- stores, one staging block after the other with at most three under way, so that copies are never far behind them
+    constexpr int kPasses = DT == ADAPTION_F32 ? 2 : 1, kUnderWay = 2;
+    int n = 0;                               // stores so far
+    for (int t = worker; ok && t < p.tiles; t += workers) {
+      const int row0 = (t % p.tiles_a) * kTile + (int)rank * kRows, col0 = (t / p.tiles_a) * kTile;
+      for (int i = 0; ok && i < kPasses * kEpiWarps; ++i, ++n) {
+        const int w = i % kEpiWarps;
+        ok = __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.staged[w]), (uint32_t)(n / kEpiWarps) & 1u, &ctrl, p));
+        if (!ok) break;
+        const int row = row0 + (w & 3) * 32, col = col0 + (w >> 2) * kWarpCols + (i / kEpiWarps) * 32;
+        if (lane == 0) {
+          if (row < p.B && col < p.cols16)
+            tma_store_2d(&map_y, ring + kStages * kStage + (uint32_t)w * kStagingBytes, col * (DT == ADAPTION_F32 ? 4 : 2), row);
+          tma_store_commit();
+          tma_store_wait_read<kUnderWay>();
+          if (n >= kUnderWay) mbar_arrive(smem_u32(&ctrl.stored[(n - kUnderWay) % kEpiWarps]));
+        }
+        __syncwarp();
+      }
+    }
+    if (lane == 0) tma_store_wait();
+    __syncwarp();
   } else if (warp >= kFirstEpiWarp) {
-    // ---- epilogue: two warps per lane quarter, each half of the columns
-    const int quarter = warp & 3, half = (warp - kFirstEpiWarp) >> 2;
-    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    // ---- epilogue: four warps per lane quarter, 64 columns each
+    const int quarter = warp & 3, part = (warp - kFirstEpiWarp) >> 2;
+    const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * kWarpCols);
+    const int self = warp - kFirstEpiWarp;
+    const uint32_t staging = ring + kStages * kStage + (uint32_t)self * kStagingBytes;
+    int blocks = 0;                          // staging blocks filled so far
     uint32_t counted = 0;
     int local = 0;
     for (int t = worker; t < p.tiles; t += workers, ++local) {
       const int ta = t % p.tiles_a, tb = t / p.tiles_a;
-      const int at = ta * kTile + (int)rank * kRows + quarter * 32 + lane;          // this lane's row of A
-      TileLane tile;
-      tile.first = tb * kTile;
-      tile.real = at < (ROWS ? p.B : p.O);
-      tile.bias = 0.f;
-      tile.biases = bias_tile;
+      const int at0 = ta * kTile + (int)rank * kRows + quarter * 32, at = at0 + lane;    // this warp's first row of A, this lane's
+      const int col = tb * kTile + part * kWarpCols;                                      // its first row of B
+      const bool real = at < (ROWS ? p.B : p.O);
+      float bias = 0.f;
       if (ROWS) {
-        tile.y = p.y + (long long)at * p.y_pitch;
         // the channels' biases; every warp has left the last tile's behind when all come here
-        const int i = (int)threadIdx.x - 32 * kFirstEpiWarp, o = tile.first + i;
+        const int i = (int)threadIdx.x - 32 * kFirstEpiWarp, o = tb * kTile + i;
         asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
-        bias_tile[i] = p.bias != nullptr && o < p.O ? __ldg(p.bias + o) : 0.f;
+        if (i < kTile) bias_tile[i] = p.bias != nullptr && o < p.O ? __ldg(p.bias + o) : 0.f;
         asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
-      } else {
-        tile.y = p.y + (long long)tile.first * p.y_pitch + (long long)at * (DT == ADAPTION_F32 ? 4 : 2);
-        if (p.bias != nullptr && tile.real) tile.bias = __ldg(p.bias + at);
+      } else if (p.bias != nullptr && real) {
+        bias = __ldg(p.bias + at);
       }
       // (a wait that ran out in one warp is seen by the others at their next one)
-      ok = ok && __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.acc_full[local & 1]), (uint32_t)(local >> 1) & 1u, &ctrl, p));
+      ok = ok && __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.acc_full), (uint32_t)local & 1u, &ctrl, p));
       if (!ok) {
         if (ROWS) continue;              // (the others still meet at the barriers)
         break;
       }
       tc_fence_after();
+      int32_t r[2][32];
+      tmem_ld32(acc, r[0]);
+      tmem_ld32(acc + 32u, r[1]);
+      tmem_ld_wait();
+      pin_after_wait32(r[0]);
+      pin_after_wait32(r[1]);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_remote(mapa_rank(smem_u32(&ctrl.acc_free), 0));
       ZeroCount<DT> zeros;
-      // the columns that the next tile's accumulator shares first: the last ones of the first accumulator, the first ones
-      // of the second; in runs of 16
-      const uint32_t acc = lanes + ((local & 1) ? kSecond : 0u);
-      const int first = (local & 1) ? 0 : (int)kSecond, rest = (local & 1) ? kShared : 0;
-      if (BLOCK == 32) {
-        if (half == 0) {
-          finish_shared<DT, ROWS, 2>(p, acc, tile, first, &ctrl, lane, zeros);
-          finish_rest<DT, ROWS, 3>(p, acc, tile, rest, zeros);
-          finish_rest<DT, ROWS, 3>(p, acc, tile, rest + 48, zeros);
-        } else {
-          finish_shared<DT, ROWS, 1>(p, acc, tile, first + 32, &ctrl, lane, zeros);
-          finish_rest<DT, ROWS, 3>(p, acc, tile, rest + 96, zeros);
-          finish_rest<DT, ROWS, 2>(p, acc, tile, rest + 144, zeros);
-          finish_rest<DT, ROWS, 2>(p, acc, tile, rest + 176, zeros);
+      if (ROWS) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (h == 0 || DT == ADAPTION_F32) {
+            // the block is free once the last store has read it
+            if (blocks > 0) ok = ok && __all_sync(0xffffffffu, pair_wait(smem_u32(&ctrl.stored[self]), (uint32_t)(blocks - 1) & 1u, &ctrl, p));
+            ++blocks;
+          }
+          if (!ok) break;
+          stage_row<DT>(p, r[h], staging, h, lane, col + 32 * h, real, p.y + (long long)at * p.y_pitch, bias_tile + part * kWarpCols + 32 * h,
+                        zeros);
+          if (h == 1 || DT == ADAPTION_F32) {
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctrl.staged[self]));
+          }
         }
-      } else {
-        finish_shared<DT, ROWS, 3>(p, acc, tile, first + 48 * half, &ctrl, lane, zeros);
-        finish_rest<DT, ROWS, 3>(p, acc, tile, rest + 80 * half, zeros);
-        finish_rest<DT, ROWS, 2>(p, acc, tile, rest + 80 * half + 48, zeros);
+      } else if (real) {
+        uint8_t* const y = p.y + (long long)col * p.y_pitch + (long long)at * (DT == ADAPTION_F32 ? 4 : 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          finish_channel<DT>(p, &r[i >> 1][16 * (i & 1)], y + (long long)(16 * i) * p.y_pitch, p.B - col - 16 * i, bias, zeros);
       }
       counted += zeros.total();
     }
@@ -475,14 +472,14 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 
 template <int BLOCK, int DT, bool ROWS>
 int launch_pair(const CUtensorMap* maps, const PairParams& p, int grid, cudaStream_t stream) {
-  const size_t smem = (size_t)p.stages * stage_bytes(BLOCK) + 1024;
+  constexpr size_t smem = smem_bytes(BLOCK);
   static std::atomic<uint64_t> prepared{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_failure(e, "fp4_pair_kernel device");
   if (dev >= 64 || !((prepared.load(std::memory_order_acquire) >> dev) & 1)) {
     e = cudaFuncSetAttribute(fp4_pair_kernel<BLOCK, DT, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)kSmemLimit);
+                             (int)smem);
     if (e != cudaSuccess) return cuda_failure(e, "fp4_pair_kernel attribute");
     if (dev < 64) prepared.fetch_or((uint64_t)1 << dev, std::memory_order_release);
   }
@@ -500,7 +497,7 @@ int launch_pair(const CUtensorMap* maps, const PairParams& p, int grid, cudaStre
   cfg.attrs = attr;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
   count_launch();
-  e = cudaLaunchKernelEx(&cfg, fp4_pair_kernel<BLOCK, DT, ROWS>, maps[0], maps[1], maps[2], maps[3], p);
+  e = cudaLaunchKernelEx(&cfg, fp4_pair_kernel<BLOCK, DT, ROWS>, maps[0], maps[1], maps[2], maps[3], maps[4], p);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return cuda_failure(e, "fp4_pair_kernel launch");
@@ -533,8 +530,8 @@ int launch_fp4_pair(const Fp4Problem& g) {
   const int size = dtype_size(g.y.dtype);
   p.y = (uint8_t*)g.y.data;
   p.y_pitch = g.y.stride * size;
-  const bool rows = aligned16(g.y.data) && (p.y_pitch & 15) == 0;
-  p.aligned32 = ((reinterpret_cast<uintptr_t>(g.y.data) | (uintptr_t)p.y_pitch) & 31u) == 0;
+  const bool rows = aligned16(g.y.data) && (p.y_pitch & 15) == 0 && (int64_t)p.O * size >= 16;
+  p.cols16 = (int)(((int64_t)p.O * size & ~(int64_t)15) / size);
   const adaption_fp4tensor &ta = rows ? g.x : g.w, &tb = rows ? g.w : g.x;
   const int na = rows ? p.B : p.O, nb = rows ? p.O : p.B;
   p.tiles_a = (na + kTile - 1) / kTile;
@@ -546,8 +543,6 @@ int launch_fp4_pair(const Fp4Problem& g) {
   const int k_last = (int)(g.K - (int64_t)(p.num_kb - 1) * kBlockElems);
   p.steps_last = (k_last + kStepElems - 1) / kStepElems;
   p.groups_last = (int)(groups - (int64_t)(p.num_kb - 1) * groups_of(block));
-  p.stages = (int)((kSmemLimit - 1024) / stage_bytes(block));
-  if (p.stages > kMaxStages) p.stages = kMaxStages;
   p.unit = pow2_float(g.x.exp + g.w.exp);
   p.bias = g.bias;
   p.relu = g.relu ? 1 : 0;
@@ -555,7 +550,8 @@ int launch_fp4_pair(const Fp4Problem& g) {
   p.timeout_ns = wait_limit_ns();
   p.stall_at = knob(kStallAt);
   if (!load_tensor_map_encoders()) return ADAPTION_ERR_CUDA;
-  CUtensorMap maps[4];
+  CUtensorMap maps[5];
+  std::memset(&maps[4], 0, sizeof(maps[4]));
   const uint64_t bytes = (uint64_t)(g.K + 1) / 2;
   bool ok = encode_tiled_2d(&maps[0], ta.codes, bytes, (uint64_t)na, (uint64_t)ta.c_stride / 2, kBlockBytes, kRows,
                             CU_TENSOR_MAP_SWIZZLE_128B) &&
@@ -568,6 +564,9 @@ int launch_fp4_pair(const Fp4Problem& g) {
     const uint32_t box[2] = {(uint32_t)(groups_of(block) * (kFp4TileBytes / 8)), i ? 2u : 1u};
     ok = encode_tiled_words(&maps[2 + i], i ? tb.scales : ta.scales, 2, dims, strides, box);
   }
+  // rows of y: boxes of 128 bytes x 32 rows
+  if (ok && rows)
+    ok = encode_tiled_2d(&maps[4], p.y, (uint64_t)p.O * (uint64_t)size & ~(uint64_t)15, (uint64_t)p.B, (uint64_t)p.y_pitch, 128u, 32u, CU_TENSOR_MAP_SWIZZLE_128B);
   if (!ok) return ADAPTION_ERR_CUDA;
   int pairs = num_sms() / 2;
   if (pairs > p.tiles) pairs = p.tiles;
