@@ -42,7 +42,6 @@ struct Fp4Problem {
 };
 int fp4_ip_impl(const Fp4Problem& p);
 // The persistent kernel over tiles of 256 channels x 256 rows (csrc/fp4_pair.cu).
-bool fp4_pair_preferred(const Fp4Problem& p);
 int launch_fp4_pair(const Fp4Problem& p);
 
 inline int dtype_size(int32_t dtype) { return dtype == ADAPTION_F32 ? 4 : 2; }

@@ -1,4 +1,5 @@
-// Inner product of microscaled 4-bit operands (adaption_fp4_ip_fwd) on the tensor cores.
+// Inner product of microscaled 4-bit operands (adaption_fp4_ip_fwd) on the tensor cores, for problems with few output tiles: one
+// thread-block cluster per tile, which shares the reduction.
 //
 //   y[b][o] = act(2^(ex + ew) sum over blocks of sx sw (sum of code products) + bias[o])
 //
@@ -9,10 +10,16 @@
 // alignment of y's rows.
 //
 // A k-block is 128 bytes of codes per row (256 elements), copied by TMA with the 128-byte swizzle, and the scale tiles of the same
-// elements (two of 512 bytes per 128 rows for blocks of 32, four for blocks of 16), which lie one after the other in memory and are copied as one
-// run.  The issuing thread moves them to TMEM (tcgen05.cp, 32 rows x 16 bytes repeated in the four lane quarters: what
+// elements (two of 512 bytes per 128 rows for blocks of 32, four for blocks of 16), which lie one after the other in memory.
+// The issuing thread moves them to TMEM (tcgen05.cp, 32 rows x 16 bytes repeated in the four lane quarters: what
 // the MMA reads) into columns that belong to the ring's stage: they are written again only after the MMAs that read
 // them have released the stage.
+//
+// Two forms: single CTAs on tiles of 128 channels x up to 128 rows, and pairs of CTAs (cta_group::2) on 256 x 256, which need two
+// thirds of the copied bytes per product.  The S CTAs (pairs) of a cluster take shares of the k-blocks; at the end each owns
+// every S-th run of four columns, sends its partial sums of the others' runs to their shared memory (st.async, counted by an
+// mbarrier there), and adds what it receives in the order of the shares.  (Read by their owners behind a cluster barrier, the
+// sums took 2500 cycles instead.)
 #include <cuda.h>
 
 #include <cstring>
@@ -29,46 +36,46 @@ namespace {
 
 constexpr int kMaxStages = 10;
 constexpr int kThreads = 256;              // warp 0: copies; 1: MMA; all of them: the epilogue
+constexpr size_t kSmemLimit = 226 * 1024;  // of 227 KB, less the control block
 
 struct FpParams {
   int O, B;                     // output channels, batch rows
-  int S;                        // CTAs per tile (cluster size)
+  int S;                        // shares of the reduction
   int tiles_o;
-  int BN;                       // columns of a tile: multiple of 16, of 128 where there are several column tiles
+  int BN;                       // columns of a tile: a multiple of 16
   int chunks_b;                 // scale tiles that cover them
   int num_kb, kb_per_split;
   int steps_last;               // MMAs of the last k-block
   int groups_last;              // scale tiles of the last k-block and 128 rows
-  int64_t groups;               // ... of all
-  int scale_tiles_b;            // rows of scale tiles of the batch
   int stages;
   uint32_t b_bytes, stage_bytes, tmem_cols, sf_col;
-  const uint8_t* sfa;
-  const uint8_t* sfb;
+  uint32_t recv_offset;         // of the received sums, in bytes from the ring's start
+  int overlay;                  // they lie in the ring
   float unit;                   // 2^(sum of the operands' exponents)
   const float* bias;
   int relu;
   void* y;
   long long y_stride;
-  int dtype;
   adaption_stats* stats;
   unsigned long long timeout_ns;
   int stall_at;                 // test aid, see adaption_debug_set
 };
 
 struct FpCtrl {
-  unsigned long long full[kMaxStages];
+  unsigned long long full[kMaxStages];     // PAIR: the leader's, bytes of both CTAs
   unsigned long long empty[kMaxStages];
   unsigned long long done;
+  unsigned long long recv;                 // the other shares' partial sums have arrived
   uint32_t tmem_base;
   volatile uint32_t abort;
 };
 
-__device__ __noinline__ bool fp_wait_slow(uint32_t bar, uint32_t parity, FpCtrl* ctrl, const FpParams& p) {
+__device__ __noinline__ bool fp_wait_slow(uint32_t bar, uint32_t parity, FpCtrl* ctrl, const FpParams& p, unsigned long long limit,
+                                          bool heed_abort) {
   const unsigned long long t0 = global_ns();
   while (!mbar_try_wait_suspend(bar, parity, 1000u)) {
-    if (ctrl->abort) return false;
-    if (global_ns() - t0 > p.timeout_ns) {
+    if (heed_abort && ctrl->abort) return false;
+    if (global_ns() - t0 > limit) {
       ctrl->abort = 1;
       atomicExch(&p.stats->status, (int)ADAPTION_ERR_TIMEOUT);
       return false;
@@ -78,60 +85,60 @@ __device__ __noinline__ bool fp_wait_slow(uint32_t bar, uint32_t parity, FpCtrl*
 }
 __device__ __forceinline__ bool fp_wait(uint32_t bar, uint32_t parity, FpCtrl* ctrl, const FpParams& p) {
   if (mbar_try_wait(bar, parity)) return true;
-  return fp_wait_slow(bar, parity, ctrl, p);
+  return fp_wait_slow(bar, parity, ctrl, p, p.timeout_ns, true);
 }
 
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
+// four floats to the shared memory of a CTA of the cluster, counted by a barrier there
+__device__ __forceinline__ void st_async_v4(uint32_t addr, uint32_t bar, int32_t a, int32_t b, int32_t c, int32_t d) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(addr), "r"(a), "r"(b),
+               "r"(c), "r"(d), "r"(bar)
+               : "memory");
 }
 
-// `n` (at most 4) consecutive outputs; returns how many are stored as 0
-__device__ __forceinline__ uint32_t store_outputs(const FpParams& p, long long at, const float (&v)[4], int n) {
+// Four outputs of one channel, `rows` of them real, in rows of y from `at` on; returns how many are stored as 0.
+template <int DT>
+__device__ __forceinline__ uint32_t store_run(const FpParams& p, long long at, const float (&v)[4], int rows) {
   uint32_t zeros = 0;
-  if (p.dtype == ADAPTION_F32) {
+  if (DT == ADAPTION_F32) {
     float* y = reinterpret_cast<float*>(p.y) + at;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) zeros += k < n && v[k] == 0.f;
-    if (n == 4 && (reinterpret_cast<uintptr_t>(y) & 15) == 0) {
-      *reinterpret_cast<float4*>(y) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < n) y[k] = v[k];
+    for (int k = 0; k < 4; ++k, y += p.y_stride) {
+      if (k < rows) {
+        *y = v[k];
+        zeros += v[k] == 0.f;
+      }
     }
-    return zeros;
-  }
-  uint32_t w[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) w[k] = p.dtype == ADAPTION_F16 ? pack2<ADAPTION_F16>(v[2 * k], v[2 * k + 1]) : pack2<ADAPTION_BF16>(v[2 * k], v[2 * k + 1]);
-  uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + at;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) zeros += k < n && ((w[k >> 1] >> (16 * (k & 1))) & 0x7fffu) == 0u;
-  if (n == 4 && (reinterpret_cast<uintptr_t>(y) & 7) == 0) {
-    *reinterpret_cast<uint2*>(y) = make_uint2(w[0], w[1]);
   } else {
+    const uint32_t w[2] = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
+    uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + at;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (k < n) y[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+    for (int k = 0; k < 4; ++k, y += p.y_stride) {
+      const uint32_t h = k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu;
+      if (k < rows) {
+        *y = (uint16_t)h;
+        zeros += (h & 0x7fffu) == 0u;
+      }
+    }
   }
   return zeros;
 }
 
-// One cluster of S CTAs per tile of 128 channels x BN batch rows: each CTA reduces its share of the k-blocks, leaves
-// its partial sums in its shared memory, and finishes the columns that fall to it from all CTAs' sums in rank order.
-template <int BLOCK>
+template <int BLOCK, bool PAIR, int DT>
 __global__ void __launch_bounds__(kThreads, 1)
-fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const FpParams p) {
+fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                   const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb, const FpParams p) {
   constexpr int kGroups = groups_of(BLOCK);
+  constexpr uint32_t kSf = (uint32_t)kGroups * kFp4TileBytes;          // scales of a k-block and 128 rows
   extern __shared__ uint8_t smem_raw[];
   __shared__ FpCtrl ctrl;
   const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
-  const uint32_t rank = p.S > 1 ? cluster_ctarank() : 0u;
-  const int tile = (int)blockIdx.x / p.S;
+  const int ctas = PAIR ? 2 * p.S : p.S;
+  const uint32_t rank = ctas > 1 ? cluster_ctarank() : 0u;
+  const int share = (int)(PAIR ? rank >> 1 : rank);                    // of the reduction
+  const uint32_t half = PAIR ? rank & 1u : 0u, leader = rank - half;   // place in the pair
+  const int tile = (int)blockIdx.x / ctas;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
@@ -139,48 +146,57 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       mbar_init(smem_u32(&ctrl.empty[s]), 1);
     }
     mbar_init(smem_u32(&ctrl.done), 1);
+    mbar_init(smem_u32(&ctrl.recv), 1);
     ctrl.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (warp == 0 && lane < 4) prefetch_map(lane == 0 ? &map_a : (lane == 1 ? &map_b : (lane == 2 ? &map_sfa : &map_sfb)));
   if (warp == 1) {
-    tmem_alloc<false>(smem_u32(&ctrl.tmem_base), p.tmem_cols);
-    tmem_relinquish<false>();
+    tmem_alloc<PAIR>(smem_u32(&ctrl.tmem_base), p.tmem_cols);
+    tmem_relinquish<PAIR>();
   }
   tc_fence_before();
   __syncthreads();
+  // the barriers exist before another CTA signals them: a pair's at once, others when sums are sent
+  if (ctas > 1) cluster_arrive();
+  if (PAIR) cluster_wait();
   tc_fence_after();
   const uint32_t tmem = ctrl.tmem_base;
 
   const int to = tile % p.tiles_o, tb = tile / p.tiles_o;
-  const int o0 = to * kRows, b0 = tb * p.BN;
-  const int kb_begin = (int)rank * p.kb_per_split;
+  const int o0 = (PAIR ? to * 2 + (int)half : to) * kRows, b0 = tb * p.BN;
+  const int cols = min(p.BN, p.B - b0), col4 = (cols + 3) / 4;         // real columns, in runs of four
+  const int runs = (col4 - share + p.S - 1) / p.S;                     // runs that this CTA finishes: share, share + S, ...
+  const int kb_begin = share * p.kb_per_split;
   const int kb_end = min(p.num_kb, kb_begin + p.kb_per_split);
 
   pdl_wait();
   pdl_launch_dependents();
 
+  // this thread's channel of the epilogue
+  const int my_row = (int)threadIdx.x & (kRows - 1), o = o0 + my_row;
+  const float bias = p.bias != nullptr && o < p.O ? __ldg(p.bias + o) : 0.f;
+
   bool ok = true;
   if (warp == 0) {
-    const int chunks = min(p.chunks_b, p.scale_tiles_b - b0 / kRows);      // scale tiles that exist
-    const uint8_t* const sfa = p.sfa + (int64_t)to * p.groups * kFp4TileBytes;
-    const uint8_t* const sfb = p.sfb + (int64_t)(b0 / kRows) * p.groups * kFp4TileBytes;
     int s = 0, issued = 0;
     uint32_t ph = 0;
+    const uint32_t issue = elect_one() ? 1u : 0u;
     for (int kb = kb_begin; kb < kb_end; ++kb) {
       if (issued == p.stall_at) break;
-      ok = __all_sync(0xffffffffu, fp_wait(smem_u32(&ctrl.empty[s]), ph ^ 1u, &ctrl, p));
-      if (!ok) break;
-      if (elect_one()) {
-        const uint32_t full = smem_u32(&ctrl.full[s]), dst = ring + (uint32_t)s * p.stage_bytes;
-        const uint32_t sf = (uint32_t)(kb == p.num_kb - 1 ? p.groups_last : kGroups) * kFp4TileBytes;
-        mbar_expect_tx(full, kABytes + p.b_bytes + sf * (uint32_t)(1 + chunks));
-        tma_load_2d<false>(dst, &map_a, full, kb * kBlockBytes, o0);
-        tma_load_2d<false>(dst + kABytes, &map_b, full, kb * kBlockBytes, b0);
-        const uint32_t at = dst + kABytes + p.b_bytes;
-        const int64_t src = (int64_t)kb * kGroups * kFp4TileBytes;
-        bulk_load(at, sfa + src, sf, full);
-        for (int c = 0; c < chunks; ++c)
-          bulk_load(at + (uint32_t)(1 + c) * (kGroups * kFp4TileBytes), sfb + (int64_t)c * p.groups * kFp4TileBytes + src, sf, full);
+      if (issued >= p.stages) {
+        ok = __all_sync(0xffffffffu, fp_wait(smem_u32(&ctrl.empty[s]), ph ^ 1u, &ctrl, p));
+        if (!ok) break;
+      }
+      if (issue) {
+        const uint32_t own = smem_u32(&ctrl.full[s]), dst = ring + (uint32_t)s * p.stage_bytes;
+        if (half == 0u) mbar_expect_tx(own, (PAIR ? 2u : 1u) * p.stage_bytes);
+        const uint32_t full = PAIR ? mapa_rank(own, leader) : own;
+        const int words = kb * kGroups * (kFp4TileBytes / 8);
+        tma_load_2d<PAIR>(dst, &map_a, full, kb * kBlockBytes, o0);
+        tma_load_2d<PAIR>(dst + kABytes, &map_b, full, kb * kBlockBytes, PAIR ? b0 + (int)half * (p.BN / 2) : b0);
+        tma_load_2d<PAIR>(dst + kABytes + p.b_bytes, &map_sfa, full, words, o0 / kRows);
+        tma_load_2d<PAIR>(dst + kABytes + p.b_bytes + kSf, &map_sfb, full, words, b0 / kRows);
       }
       __syncwarp();
       ++issued;
@@ -189,53 +205,61 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     // the ring is given another use only once the MMAs (or the issuing warp, giving up) are through with it
     if (!fp_wait(smem_u32(&ctrl.done), 0, &ctrl, p)) ok = false;
     if ((!ok || ctrl.abort) && lane == 0) {
-      // gave up: let the copies in flight land
+      // gave up: let the copies in flight land.  (A pair's bytes are counted on the leader's barriers: the follower just waits.)
       const int n = issued < p.stages ? issued : p.stages;
+      const unsigned long long t0 = global_ns();
       for (int j = issued - n; j < issued; ++j) {
-        const unsigned long long t0 = global_ns();
-        while (!mbar_try_wait(smem_u32(&ctrl.full[j % p.stages]), (uint32_t)(j / p.stages) & 1u) &&
-               global_ns() - t0 < 5000000ull) {
+        while (global_ns() - t0 < 5000000ull &&
+               (half != 0u || !mbar_try_wait(smem_u32(&ctrl.full[j % p.stages]), (uint32_t)(j / p.stages) & 1u))) {
         }
       }
     }
     __syncwarp();
-  } else if (warp == 1) {
+  } else if (warp == 1 && half == 0u) {
     const uint32_t issue = elect_one() ? 1u : 0u;
-    const uint32_t id = make_idesc_fp4(BLOCK, p.BN, kRows);
+    const uint32_t id = make_idesc_fp4(BLOCK, p.BN, PAIR ? 2 * kRows : kRows);
     const uint32_t dhi = smem_desc_hi(8u * kBlockBytes, 2u);          // 128-byte swizzle
     const uint32_t shi = smem_desc_hi(128u, 0u);                       // scale tiles: rows of 16 bytes, groups of 8 rows
-    const uint32_t cols_b = 4u * (uint32_t)p.chunks_b;
-    const uint32_t slot = (uint32_t)kGroups * (4u + cols_b);
+    const uint32_t cols_b = 4u * (uint32_t)p.chunks_b, slot = (uint32_t)kGroups * (4u + cols_b);
+    const uint16_t mask = (uint16_t)(3u << leader);
     int s = 0;
     uint32_t ph = 0;
+    bool full_next = false;
     for (int kb = kb_begin; kb < kb_end; ++kb) {
-      ok = __all_sync(0xffffffffu, fp_wait(smem_u32(&ctrl.full[s]), ph, &ctrl, p));
+      // (looked at while the k-block before was issued)
+      if (!full_next) ok = __all_sync(0xffffffffu, fp_wait(smem_u32(&ctrl.full[s]), ph, &ctrl, p));
       if (!ok) break;
+      const int next_s = s + 1 == p.stages ? 0 : s + 1;
+      const uint32_t next_ph = next_s == 0 ? ph ^ 1u : ph;
+      full_next = __all_sync(0xffffffffu, mbar_test(smem_u32(&ctrl.full[next_s]), next_ph));
       tc_fence_after();
-      const bool last = kb == p.num_kb - 1;
-      const int steps = last ? p.steps_last : kBlockElems / kStepElems, groups = last ? p.groups_last : kGroups;
       const uint32_t a = smem_desc_lo(ring) + (uint32_t)s * (p.stage_bytes >> 4), b = a + (kABytes >> 4);
       const uint32_t sf = ((ring + (uint32_t)s * p.stage_bytes + kABytes + p.b_bytes) >> 4) & 0x3FFFu;
-      const uint32_t ta = tmem + p.sf_col + (uint32_t)s * slot, tbx = ta + 4u * kGroups;
+      const uint32_t ta = tmem + p.sf_col + (uint32_t)s * slot, tb0 = ta + 4u * kGroups;
+      const bool last = kb == p.num_kb - 1;
+      const int steps = last ? p.steps_last : kBlockElems / kStepElems, groups = last ? p.groups_last : kGroups;
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         if (g < groups) {
-          scales_to_tmem<false>(issue, ta + 4u * g, sf + 32u * g, shi);
-          scales_to_tmem<false>(issue, tbx + cols_b * g, sf + 32u * (uint32_t)(kGroups + g), shi);
-          if (p.chunks_b > 1) scales_to_tmem<false>(issue, tbx + cols_b * g + 4u, sf + 32u * (uint32_t)(2 * kGroups + g), shi);
+          scales_to_tmem<PAIR>(issue, ta + 4u * g, sf + 32u * g, shi);
+          scales_to_tmem<PAIR>(issue, tb0 + cols_b * g, sf + 32u * (kGroups + g), shi);
+          if (PAIR && p.chunks_b > 1) scales_to_tmem<PAIR>(issue, tb0 + cols_b * g + 4u, sf + 32u * (2 * kGroups + g), shi);
         }
       }
 #pragma unroll
       for (int k = 0; k < kBlockElems / kStepElems; ++k) {
         const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
         if (k < steps)
-          mma_fp4<BLOCK, false>(issue, tmem, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g,
-                                tbx + cols_b * g, (kb > kb_begin || k > 0) ? 1u : 0u);
+          mma_fp4<BLOCK, PAIR>(issue, tmem, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g,
+                               tb0 + cols_b * g, (kb > kb_begin || k > 0) ? 1u : 0u);
       }
-      tc_commit_if<false>(issue, smem_u32(&ctrl.empty[s]));
-      if (++s == p.stages) { s = 0; ph ^= 1u; }
+      if (PAIR) commit_pair_if(issue, smem_u32(&ctrl.empty[s]), mask);
+      else tc_commit_if<false>(issue, smem_u32(&ctrl.empty[s]));
+      s = next_s;
+      ph = next_ph;
     }
-    if (elect_one()) tc_commit<false>(smem_u32(&ctrl.done));
+    if (PAIR) commit_pair_if(issue, smem_u32(&ctrl.done), mask);
+    else tc_commit_if<false>(issue, smem_u32(&ctrl.done));
     __syncwarp();
     if (!ok || ctrl.abort) {
       // no MMA may still read shared memory when the ring is given another use
@@ -245,66 +269,93 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     }
   }
   __syncwarp();
+
+  // ---- partial sums to their owners: recv[share][run of the owner][128 channels] of 16 bytes
+  if (threadIdx.x == 0 && p.S > 1 && runs > 0) mbar_expect_tx(smem_u32(&ctrl.recv), (uint32_t)(p.S - 1) * (uint32_t)runs * (kRows * 16u));
+  // (warps 2.. wait here for the MMAs, and in a pair the follower's for the leader's)
+  ok = fp_wait(smem_u32(&ctrl.done), 0, &ctrl, p) && ok;
   __syncthreads();
-  const int cols = min(p.BN, p.B - b0);
-  // partial sums to shared memory: [column][128 channels]
-  float* const part = reinterpret_cast<float*>(smem_raw + (ring - smem_u32(smem_raw)));
+  if (ctas > 1) {
+    if (!PAIR) cluster_wait();                        // (arrived at the start: long complete)
+    if (p.overlay) cluster_sync_all();                // every CTA's ring has come to its end
+  }
+  const uint32_t recv = ring + p.recv_offset, part_bytes = (uint32_t)((col4 + p.S - 1) / p.S) * (kRows * 16u);     // of one share
   {
     tc_fence_after();
     const int quarter = warp & 3, row = quarter * 32 + lane;
-    for (int c = 8 * (warp >> 2); c < cols; c += 8 * (kThreads / 128)) {
-      int32_t a[8];
-      tmem_ld8(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, a);
+    const uint32_t local = recv + (uint32_t)share * part_bytes + (uint32_t)row * 16u, recv_bar = smem_u32(&ctrl.recv);
+    const bool empty = kb_begin >= kb_end;            // (no k-blocks: the accumulator was never written)
+    for (int c = 16 * (warp >> 2); c < cols; c += 16 * (kThreads / 128)) {
+      int32_t r[2][8];
+      tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, r[0], r[1]);
       tmem_ld_wait();
-      pin_after_wait(a);
-      // (a CTA without k-blocks has no sums: its accumulator was never written)
+      pin_after_wait(r[0]);
+      pin_after_wait(r[1]);
+      int owner = (c >> 2) % p.S, place = (c >> 2) / p.S;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) part[(c + j) * kRows + row] = kb_begin < kb_end ? __int_as_float(a[j]) : 0.f;
+      for (int j = 0; j < 4; ++j) {
+        if (c + 4 * j >= cols) break;
+        int32_t* v = &r[j >> 1][4 * (j & 1)];
+        if (empty) v[0] = v[1] = v[2] = v[3] = 0;
+        const uint32_t at = local + (uint32_t)place * (kRows * 16u);
+        if (owner == share) {
+          st_shared_v4(at, (uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]);
+        } else {
+          const uint32_t to_rank = PAIR ? 2u * (uint32_t)owner + half : (uint32_t)owner;
+          st_async_v4(mapa_rank(at, to_rank), mapa_rank(recv_bar, to_rank), v[0], v[1], v[2], v[3]);
+        }
+        if (++owner == p.S) { owner = 0; ++place; }
+      }
     }
     tc_fence_before();
   }
-  if (p.S > 1) cluster_sync_all();
-  else __syncthreads();
+  __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc<false>(tmem, p.tmem_cols);
+    tmem_dealloc<PAIR>(tmem, p.tmem_cols);
   }
+  // Every CTA of the cluster sends, also one that gave up (within its waits' limits), so this wait ends, and no CTA leaves while
+  // sums for it are under way.
+  if (p.S > 1 && runs > 0 && !mbar_try_wait(smem_u32(&ctrl.recv), 0))
+    ok = fp_wait_slow(smem_u32(&ctrl.recv), 0, &ctrl, p, 4ull * p.timeout_ns + 1000000000ull, false) && ok;
+
+  // ---- the runs this CTA owns: sum over the shares, bias, ReLU, store
   uint32_t zeros = 0;
-  if (!ctrl.abort) {
-    const uint32_t base = smem_u32(part);
-    for (int c = (int)rank + p.S * warp; c < cols; c += p.S * (kThreads / 32)) {
-      const uint32_t at = base + (uint32_t)(c * kRows + 4 * lane) * 4u;
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int r = 0; r < p.S; ++r) {
-        const float4 t = p.S > 1 ? ld_cluster_f4(mapa_rank(at, (uint32_t)r))
-                                 : *reinterpret_cast<const float4*>(part + c * kRows + 4 * lane);
-        v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
-      }
-      const int o = o0 + 4 * lane, n = min(4, p.O - o);
+  if (ok && o < p.O && !ctrl.abort) {
+    for (int i = (int)threadIdx.x / kRows; i < runs; i += kThreads / kRows) {
+      const uint32_t at = recv + (uint32_t)i * (kRows * 16u) + (uint32_t)my_row * 16u;
+      float4 part[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k < p.S) part[k] = ld_shared_f4(at + (uint32_t)k * part_bytes);
+      float v[4] = {part[0].x, part[0].y, part[0].z, part[0].w};
+#pragma unroll
+      for (int k = 1; k < 8; ++k)
+        if (k < p.S) { v[0] += part[k].x; v[1] += part[k].y; v[2] += part[k].z; v[3] += part[k].w; }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        v[k] = fmaf(v[k], p.unit, p.bias != nullptr && k < n ? __ldg(p.bias + o + k) : 0.f);
+        v[k] = fmaf(v[k], p.unit, bias);
         if (p.relu) v[k] = v[k] < 0.f ? 0.f : v[k];
       }
-      if (n > 0) zeros += store_outputs(p, (long long)(b0 + c) * p.y_stride + o, v, n);
+      const int c = 4 * (share + i * p.S);
+      zeros += store_run<DT>(p, (long long)(b0 + c) * p.y_stride + o, v, cols - c);
     }
   }
   __syncwarp();
   zeros = __reduce_add_sync(0xffffffffu, zeros);
   if (lane == 0 && zeros) atomicAdd((unsigned long long*)&p.stats->zeros, (unsigned long long)zeros);
-  if (p.S > 1) cluster_sync_all();        // (peers may still read this CTA's sums)
+  // (a pair frees TMEM together: neither leaves before the other is that far)
+  if (PAIR) cluster_sync_all();
 }
 
-constexpr size_t kSmemLimit = 227 * 1024 - 512;      // less the control block
-
-template <int BLOCK>
-int launch_cluster_fp4(const CUtensorMap& ma, const CUtensorMap& mb, const FpParams& p, int grid, size_t smem, cudaStream_t stream) {
+template <int BLOCK, bool PAIR, int DT>
+int launch_cluster(const CUtensorMap* maps, const FpParams& p, int grid, size_t smem, cudaStream_t stream) {
   static std::atomic<uint64_t> prepared{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_failure(e, "fp4_cluster_kernel device");
   if (dev >= 64 || !((prepared.load(std::memory_order_acquire) >> dev) & 1)) {
-    e = cudaFuncSetAttribute(fp4_cluster_kernel<BLOCK>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
+    e = cudaFuncSetAttribute(fp4_cluster_kernel<BLOCK, PAIR, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
     if (e != cudaSuccess) return cuda_failure(e, "fp4_cluster_kernel attribute");
     if (dev < 64) prepared.fetch_or((uint64_t)1 << dev, std::memory_order_release);
   }
@@ -315,9 +366,10 @@ int launch_cluster_fp4(const CUtensorMap& ma, const CUtensorMap& mb, const FpPar
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   int n = 0;
-  if (p.S > 1) {
+  const int ctas = PAIR ? 2 * p.S : p.S;
+  if (ctas > 1) {
     attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = (unsigned)p.S;
+    attr[n].val.clusterDim.x = (unsigned)ctas;
     attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
     ++n;
   }
@@ -329,7 +381,7 @@ int launch_cluster_fp4(const CUtensorMap& ma, const CUtensorMap& mb, const FpPar
   cfg.attrs = n ? attr : nullptr;
   cfg.numAttrs = (unsigned)n;
   count_launch();
-  e = cudaLaunchKernelEx(&cfg, fp4_cluster_kernel<BLOCK>, ma, mb, p);
+  e = cudaLaunchKernelEx(&cfg, fp4_cluster_kernel<BLOCK, PAIR, DT>, maps[0], maps[1], maps[2], maps[3], p);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return cuda_failure(e, "fp4_cluster_kernel launch");
@@ -337,70 +389,166 @@ int launch_cluster_fp4(const CUtensorMap& ma, const CUtensorMap& mb, const FpPar
   return ADAPTION_OK;
 }
 
-}  // namespace
+template <int BLOCK, bool PAIR>
+int launch_cluster(const CUtensorMap* maps, const FpParams& p, int dtype, int grid, size_t smem, cudaStream_t stream) {
+  if (dtype == ADAPTION_F32) return launch_cluster<BLOCK, PAIR, ADAPTION_F32>(maps, p, grid, smem, stream);
+  if (dtype == ADAPTION_F16) return launch_cluster<BLOCK, PAIR, ADAPTION_F16>(maps, p, grid, smem, stream);
+  return launch_cluster<BLOCK, PAIR, ADAPTION_BF16>(maps, p, grid, smem, stream);
+}
 
-static int launch_fp4_cluster(const Fp4Problem& g) {
+// Clusters of `ctas` blocks, one block per SM, that the current device runs at a time.  (A cluster stays inside one group of SMs, so
+// there are fewer than SMs / ctas: 74 of 2, 33 of 4, 22 of 6, 15 of 8 on 148 SMs.)  Asked once per device and size.
+int max_clusters(int ctas) {
+  constexpr int kMaxDevices = 64, kMaxCtas = 8;
+  static std::atomic<int> known[kMaxDevices][kMaxCtas + 1];
+  if (ctas == 1) return num_sms();
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return num_sms() / ctas;
+  if (dev < kMaxDevices) {
+    const int n = known[dev][ctas].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+  }
+  int n = 0;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemLimit;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)ctas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const auto kernel = fp4_cluster_kernel<16, true, ADAPTION_BF16>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
+    (void)cudaGetLastError();
+    n = num_sms() / (ctas > 4 ? ctas + 1 : ctas);
+    if (n < 1) n = 1;
+  }
+  if (dev < kMaxDevices) known[dev][ctas].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+struct FpPlan {
+  bool pair = false, persistent = false;
+  int S = 1;
+  double cycles = 1e300;
+};
+
+// Estimated cycles, from measured parts: an SM takes 64 bytes of copies a cycle at most, an MMA of N columns N / 2 cycles (at least
+// 40), a k-block 240 more where nothing hides the issue; 5000 for the first copies, the exchange and the end.
+FpPlan make_plan(const Fp4Problem& g, int only_pair) {
+  FpPlan best;
+  const int sms = num_sms(), kb = (int)((g.K + kBlockElems - 1) / kBlockElems), sf = groups_of(g.w.block) * kFp4TileBytes;
+  for (int pair = 0; pair < 2; ++pair) {
+    if (only_pair >= 0 && pair != only_pair) continue;
+    const int tile_o = pair ? 2 * kRows : kRows, per = pair ? 2 : 1;
+    const int64_t bn = g.B < tile_o ? (g.B + 15) / 16 * 16 : tile_o;
+    const int64_t tiles = ((g.O + tile_o - 1) / tile_o) * ((g.B + bn - 1) / bn);
+    const double bytes = (double)kABytes + (double)bn / per * kBlockBytes + (double)sf * (1 + (double)((bn + kRows - 1) / kRows));
+    const double mma = 4.0 * (bn > 80 ? (double)bn / 2 : 40.0);
+    const double block = bytes / 64 > mma ? bytes / 64 : mma, out = 12.0 * (double)bn;
+    for (int S = 1; S * per <= 8 && S <= kb; ++S) {
+      const int64_t at_once = max_clusters(S * per);
+      const double waves = (double)((tiles + at_once - 1) / at_once);
+      const double cycles = waves * ((double)((kb + S - 1) / S) * block + 5000.0 + out);
+      if (cycles < best.cycles * 0.97) {          // (more shares only where they are worth it)
+        best.pair = pair != 0;
+        best.S = S;
+        best.cycles = cycles;
+      }
+    }
+  }
+  if (only_pair < 0 && g.B > kRows) {
+    // the persistent kernel: tiles of 256 x 256 in turn, the stores of all but the last behind the next one's main loop
+    const int64_t tiles = ((g.O + 255) / 256) * ((g.B + 255) / 256), pairs = sms / 2;
+    const double bytes = 2.0 * kABytes + 3.0 * sf, block = bytes / 64 > 512 ? bytes / 64 : 512;
+    double tile = kb * block + 900.0;
+    if (tile < 4000.0) tile = 4000.0;
+    const double cycles = (double)((tiles + pairs - 1) / pairs) * tile + 8000.0;
+    if (cycles < best.cycles) {
+      best.persistent = true;
+      best.cycles = cycles;
+    }
+  }
+  return best;
+}
+
+int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
+  const bool pair = plan.pair;
   const int block = g.w.block, kgroups = groups_of(block);
   FpParams p;
   std::memset(&p, 0, sizeof(p));
   p.O = (int)g.O;
   p.B = (int)g.B;
-  p.tiles_o = (p.O + kRows - 1) / kRows;
-  p.BN = p.B <= 256 ? (p.B + 15) / 16 * 16 : 256;
-  const int tiles_b = (p.B + p.BN - 1) / p.BN;
+  const int tile_o = pair ? 2 * kRows : kRows, most = pair ? 2 * kRows : kRows;
+  p.tiles_o = (p.O + tile_o - 1) / tile_o;
+  // (several column tiles: whole scale tiles each; a pair's half of the columns is a multiple of 8)
+  p.BN = p.B < most ? (p.B + 15) / 16 * 16 : most;
+  const int64_t tiles = (int64_t)p.tiles_o * ((p.B + p.BN - 1) / p.BN);
   p.chunks_b = (p.BN + kRows - 1) / kRows;
   p.num_kb = (int)((g.K + kBlockElems - 1) / kBlockElems);
   const int k_last = (int)(g.K - (int64_t)(p.num_kb - 1) * kBlockElems);
   p.steps_last = (k_last + kStepElems - 1) / kStepElems;
-  p.groups = fp4_groups(g.K, block);
-  p.groups_last = (int)(p.groups - (int64_t)(p.num_kb - 1) * kgroups);
-  p.scale_tiles_b = (p.B + kRows - 1) / kRows;
-  const int64_t tiles = (int64_t)p.tiles_o * tiles_b;
-  p.S = 1;
-  while (p.S < 8 && tiles * p.S * 2 <= num_sms() && p.num_kb >= p.S * 2) p.S *= 2;
+  const int64_t groups = fp4_groups(g.K, block);
+  p.groups_last = (int)(groups - (int64_t)(p.num_kb - 1) * kgroups);
+  const int per = pair ? 2 : 1;
+  p.S = plan.S;
   p.kb_per_split = (p.num_kb + p.S - 1) / p.S;
-  if (tiles * p.S > 0x7fffffff) return ADAPTION_ERR_UNSUPPORTED;
-  p.b_bytes = (uint32_t)p.BN * kBlockBytes;
+  if (tiles * per * p.S > 0x7fffffff) return ADAPTION_ERR_UNSUPPORTED;
+  const int b_rows = pair ? p.BN / 2 : p.BN;
+  p.b_bytes = (uint32_t)b_rows * kBlockBytes;
   p.stage_bytes = kABytes + p.b_bytes + (uint32_t)(kgroups * kFp4TileBytes * (1 + p.chunks_b));
-  const size_t sums = (size_t)p.BN * kRows * sizeof(float);
-  int stages = (int)((kSmemLimit - 1024) / p.stage_bytes);
-  if (stages > kMaxStages) stages = kMaxStages;
-  if (stages > p.kb_per_split) stages = p.kb_per_split;
+  const int col4 = ((p.BN < p.B ? p.BN : p.B) + 3) / 4;
+  const size_t sums = (size_t)((col4 + p.S - 1) / p.S) * p.S * 16 * kRows;            // of all shares, for one owner
   p.sf_col = (uint32_t)(p.BN + 31) / 32 * 32;
   const uint32_t slot = (uint32_t)kgroups * 4u * (uint32_t)(1 + p.chunks_b);
+  // the ring has a place of its own beside the sums unless that leaves it too short
+  p.overlay = 2 * sums > kSmemLimit ? 1 : 0;
+  const size_t room = kSmemLimit - 1024 - (p.overlay ? 0 : sums);
+  int stages = (int)(room / p.stage_bytes);
+  if (stages > kMaxStages) stages = kMaxStages;
+  if (stages > p.kb_per_split) stages = p.kb_per_split;
   while (stages > 1 && p.sf_col + (uint32_t)stages * slot > 512u) --stages;
   p.stages = stages;
   p.tmem_cols = 32;
   while (p.tmem_cols < p.sf_col + (uint32_t)stages * slot) p.tmem_cols *= 2;
   size_t smem = (size_t)stages * p.stage_bytes;
-  if (smem < sums) smem = sums;
+  p.recv_offset = p.overlay ? 0u : (uint32_t)smem;
+  if (!p.overlay) smem += sums;
+  else if (smem < sums) smem = sums;
   smem += 1024;
-  p.sfa = (const uint8_t*)g.w.scales;
-  p.sfb = (const uint8_t*)g.x.scales;
   p.unit = pow2_float(g.x.exp + g.w.exp);
   p.bias = g.bias;
   p.relu = g.relu ? 1 : 0;
   p.y = g.y.data;
   p.y_stride = g.y.stride;
-  p.dtype = g.y.dtype;
   p.stats = g.stats;
   p.timeout_ns = wait_limit_ns();
   p.stall_at = knob(kStallAt);
   if (!load_tensor_map_encoders()) return ADAPTION_ERR_CUDA;
-  CUtensorMap ma, mb;
-  const uint64_t bytes = (uint64_t)(g.K + 1) / 2;
-  if (!encode_tiled_2d(&ma, g.w.codes, bytes, (uint64_t)p.O, (uint64_t)g.w.c_stride / 2, kBlockBytes, kRows,
-                       CU_TENSOR_MAP_SWIZZLE_128B, true) ||
-      !encode_tiled_2d(&mb, g.x.codes, bytes, (uint64_t)p.B, (uint64_t)g.x.c_stride / 2, kBlockBytes, (uint32_t)p.BN,
-                       CU_TENSOR_MAP_SWIZZLE_128B))
+  CUtensorMap maps[4];
+  if (!encode_fp4_codes(&maps[0], g.w, p.O, g.K, kRows, true) || !encode_fp4_codes(&maps[1], g.x, p.B, g.K, (uint32_t)b_rows, false) ||
+      !encode_fp4_scales(&maps[2], g.w, p.O, groups, 1) || !encode_fp4_scales(&maps[3], g.x, p.B, groups, (uint32_t)p.chunks_b))
     return ADAPTION_ERR_CUDA;
-  const int grid = (int)(tiles * p.S);
-  return block == 32 ? launch_cluster_fp4<32>(ma, mb, p, grid, smem, g.stream)
-                     : launch_cluster_fp4<16>(ma, mb, p, grid, smem, g.stream);
+  const int grid = (int)(tiles * per * p.S);
+  const int dtype = g.y.dtype;
+  if (pair)
+    return block == 32 ? launch_cluster<32, true>(maps, p, dtype, grid, smem, g.stream) : launch_cluster<16, true>(maps, p, dtype, grid, smem, g.stream);
+  return block == 32 ? launch_cluster<32, false>(maps, p, dtype, grid, smem, g.stream) : launch_cluster<16, false>(maps, p, dtype, grid, smem, g.stream);
 }
 
+}  // namespace
+
 int fp4_ip_impl(const Fp4Problem& g) {
-  return fp4_pair_preferred(g) ? launch_fp4_pair(g) : launch_fp4_cluster(g);
+  // (tests: one cluster per tile of single CTAs or of pairs, or the persistent kernel, wherever the call would run)
+  const int pair = knob(kPair);
+  if (pair == 1 && knob(kCluster) != 2) return launch_fp4_pair(g);
+  FpPlan plan = make_plan(g, pair);
+  const int shares = knob(kClusterSize) / (plan.pair ? 2 : 1), most = plan.pair ? 4 : 8;
+  if (shares > 0) plan.S = shares < most ? shares : most;
+  return plan.persistent ? launch_fp4_pair(g) : launch_fp4_cluster(g, plan);
 }
 
 }  // namespace adaption

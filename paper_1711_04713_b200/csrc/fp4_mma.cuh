@@ -3,6 +3,7 @@
 
 #include "fp4.cuh"
 #include "tc_ptx.cuh"
+#include "tensor_maps.cuh"
 
 namespace adaption {
 namespace {
@@ -37,12 +38,6 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// contiguous bytes of global memory -> this CTA's shared memory
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(bar)
-               : "memory");
-}
 // A box from shared memory to global memory, clipped at the tensor's ends; completion by groups of the issuing thread.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y)
@@ -55,6 +50,22 @@ __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.b
 __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+// Arrival in the CTAs of `mask` once every instruction issued so far for the pair has retired.
+__device__ __forceinline__ void commit_pair_if(uint32_t issue, uint32_t bar, uint16_t mask) {
+  asm volatile(
+      "{\n"
+      ".reg .pred e;\n"
+      "setp.ne.b32 e, %2, 0;\n"
+      "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n"
+      "}\n" ::"r"(bar),
+      "h"(mask), "r"(issue)
+      : "memory");
 }
 // The issuing warp stays in uniform control flow and the lane with `issue` != 0 (elect_one, once) executes: operands live in
 // uniform registers that way.  (In a branch of the elected lane, the sixteen instructions of a k-block of blocks of 16 took 700
@@ -114,6 +125,19 @@ __device__ __forceinline__ uint32_t make_idesc_fp4(int block, int n, int m) {
 // ... which two of the four scales of a TMEM word an instruction takes (blocks of 32): bytes 2 * half on
 __device__ __forceinline__ uint32_t scale_half(uint32_t half) { return (half * 2u) << 4 | (half * 2u) << 29; }
 
+
+// Codes: boxes of a k-block of `box_rows` rows.  A row ends with its last element's byte: what the box holds behind it arrives as zeros.
+inline bool encode_fp4_codes(CUtensorMap* map, const adaption_fp4tensor& t, int64_t rows, int64_t inner, uint32_t box_rows, bool long_rows) {
+  return encode_tiled_2d(map, t.codes, (uint64_t)(inner + 1) / 2, (uint64_t)rows, (uint64_t)t.c_stride / 2, kBlockBytes, box_rows,
+                         CU_TENSOR_MAP_SWIZZLE_128B, long_rows);
+}
+// Scale planes: one row per row of scale tiles, in words of 8 bytes; boxes of a k-block of `box_tiles` rows of tiles.
+inline bool encode_fp4_scales(CUtensorMap* map, const adaption_fp4tensor& t, int64_t rows, int64_t groups, uint32_t box_tiles) {
+  const uint64_t dims[2] = {(uint64_t)groups * (kFp4TileBytes / 8), (uint64_t)((rows + kRows - 1) / kRows)};
+  const uint64_t strides[1] = {(uint64_t)groups * kFp4TileBytes};
+  const uint32_t box[2] = {(uint32_t)(groups_of(t.block) * (kFp4TileBytes / 8)), box_tiles};
+  return encode_tiled_words(map, t.scales, 2, dims, strides, box);
+}
 
 }  // namespace
 }  // namespace adaption

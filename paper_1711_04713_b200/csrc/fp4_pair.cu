@@ -23,7 +23,6 @@
 
 #include "fp4_mma.cuh"
 #include "knobs.cuh"
-#include "tensor_maps.cuh"
 
 namespace adaption {
 
@@ -514,13 +513,6 @@ int launch_pair(const CUtensorMap* maps, const PairParams& p, int dtype, int gri
 
 }  // namespace
 
-bool fp4_pair_preferred(const Fp4Problem& g) {
-  const int mode = knob(kPair);
-  if (mode >= 0) return mode != 0;
-  const int64_t tiles = ((g.O + kTile - 1) / kTile) * ((g.B + kTile - 1) / kTile);
-  return g.B > 128 && tiles >= num_sms() / 2;
-}
-
 int launch_fp4_pair(const Fp4Problem& g) {
   const int block = g.w.block;
   PairParams p;
@@ -552,18 +544,8 @@ int launch_fp4_pair(const Fp4Problem& g) {
   if (!load_tensor_map_encoders()) return ADAPTION_ERR_CUDA;
   CUtensorMap maps[5];
   std::memset(&maps[4], 0, sizeof(maps[4]));
-  const uint64_t bytes = (uint64_t)(g.K + 1) / 2;
-  bool ok = encode_tiled_2d(&maps[0], ta.codes, bytes, (uint64_t)na, (uint64_t)ta.c_stride / 2, kBlockBytes, kRows,
-                            CU_TENSOR_MAP_SWIZZLE_128B) &&
-            encode_tiled_2d(&maps[1], tb.codes, bytes, (uint64_t)nb, (uint64_t)tb.c_stride / 2, kBlockBytes, kRows,
-                            CU_TENSOR_MAP_SWIZZLE_128B);
-  // scale planes: one row per row of tiles, in words of 8 bytes; what lies behind the last tile arrives as zeros
-  for (int i = 0; ok && i < 2; ++i) {
-    const uint64_t dims[2] = {(uint64_t)groups * (kFp4TileBytes / 8), (uint64_t)(((i ? nb : na) + kRows - 1) / kRows)};
-    const uint64_t strides[1] = {(uint64_t)groups * kFp4TileBytes};
-    const uint32_t box[2] = {(uint32_t)(groups_of(block) * (kFp4TileBytes / 8)), i ? 2u : 1u};
-    ok = encode_tiled_words(&maps[2 + i], i ? tb.scales : ta.scales, 2, dims, strides, box);
-  }
+  bool ok = encode_fp4_codes(&maps[0], ta, na, g.K, kRows, false) && encode_fp4_codes(&maps[1], tb, nb, g.K, kRows, false) &&
+            encode_fp4_scales(&maps[2], ta, na, groups, 1) && encode_fp4_scales(&maps[3], tb, nb, groups, 2);
   // rows of y: boxes of 128 bytes x 32 rows
   if (ok && rows)
     ok = encode_tiled_2d(&maps[4], p.y, (uint64_t)p.O * (uint64_t)size & ~(uint64_t)15, (uint64_t)p.B, (uint64_t)p.y_pitch, 128u, 32u, CU_TENSOR_MAP_SWIZZLE_128B);

@@ -193,15 +193,17 @@ def check_product(y, xv, wv, bias, relu, block, dtype, cols=None):
 
 
 def choose(kernel):
-    """One cluster of CTAs per tile, or the persistent kernel over pairs of CTAs, wherever the call would run."""
-    B.adaption_debug_set("pair", {"cluster": 0, "pair": 1}[kernel])
+    """One cluster of CTAs or of pairs of CTAs per tile, or the persistent kernel over pairs, wherever the call would run."""
+    if kernel != "chosen":
+        B.adaption_debug_set("pair", {"cluster": 0, "pairs": 1, "persistent": 1}[kernel])
+        B.adaption_debug_set("cluster", {"cluster": 2, "pairs": 2, "persistent": 1}[kernel])
 
 
 IP_SHAPES = [(1, 1, 1), (1, 64, 128), (1, 4096, 300), (5, 300, 130), (16, 257, 129), (17, 1000, 64), (64, 2048, 256), (100, 33, 500),
              (128, 512, 128), (129, 640, 140), (200, 1411, 257), (256, 768, 200), (257, 256, 128), (300, 900, 384), (520, 320, 1000)]
 
 
-@pytest.mark.parametrize("kernel", ["cluster", "pair"])
+@pytest.mark.parametrize("kernel", ["cluster", "pairs", "persistent"])
 @pytest.mark.parametrize("block", [16, 32])
 @pytest.mark.parametrize("shape", IP_SHAPES)
 def test_inner_product(shape, block, kernel):
@@ -224,7 +226,7 @@ def test_inner_product(shape, block, kernel):
         assert s.status == 0 and s.zeros == int((y == 0).sum())
 
 
-@pytest.mark.parametrize("kernel", ["cluster", "pair"])
+@pytest.mark.parametrize("kernel", ["cluster", "pairs", "persistent"])
 @pytest.mark.parametrize("block", [16, 32])
 def test_inner_product_of_exact_sums(block, kernel):
     """Steps of 1 (and of 2 and 1/2): every partial sum is a multiple of 1/16 below 2^20, so the result is exact, and
@@ -242,6 +244,22 @@ def test_inner_product_of_exact_sums(block, kernel):
         y = torch.empty(Bn, O, device="cuda")
         B.adaption_fp4_ip_fwd(Bn, K, O, ops[0][0], ops[1][0], None, False, y, B.new_stats())
         assert np.array_equal(y.double().cpu().numpy(), ms.inner_product(ops[0][1], ops[1][1]))
+
+
+@pytest.mark.parametrize("kernel,sizes", [("cluster", range(1, 9)), ("pairs", (2, 4, 6, 8))])
+def test_every_number_of_shares(kernel, sizes):
+    """A reduction cut into 1 to 8 shares, some of them empty, some CTAs without columns of their own."""
+    rng = np.random.default_rng(9)
+    for Bn, K, O in ((1, 700, 200), (18, 2300, 130), (130, 1500, 300)):
+        x, xv = operand(rng, Bn, K, 16)
+        w, wv = operand(rng, O, K, 16)
+        for size in sizes:
+            choose(kernel)
+            B.adaption_debug_set("cluster_size", size)
+            y, st = torch.full((Bn, O), 7.0, device="cuda"), B.new_stats()
+            B.adaption_fp4_ip_fwd(Bn, K, O, x, w, None, False, y, st)
+            check_product(y, xv, wv, None, False, 16, "f32")
+            assert B.read_stats(st).status == 0
 
 
 @pytest.mark.parametrize("block", [16, 32])
@@ -292,7 +310,7 @@ def test_product_of_real_activations(block):
         assert s.status == 0 and s.zeros == 2 * int((y == 0).sum())
 
 
-@pytest.mark.parametrize("kernel", ["cluster", "pair"])
+@pytest.mark.parametrize("kernel", ["cluster", "pairs", "persistent"])
 def test_infinite_and_nan_results_stay_in_their_places(kernel):
     """A NaN scale of one row or one channel reaches that row or channel alone; ReLU keeps NaN; fp16 results beyond its range are infinite."""
     choose(kernel)
@@ -421,7 +439,7 @@ def test_refusals_of_the_binding():
     torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("kernel", ["cluster", "pair"])
+@pytest.mark.parametrize("kernel", ["cluster", "pairs", "persistent"])
 @pytest.mark.parametrize("Bn", [4, 300])
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(Bn, kernel):
     choose(kernel)
