@@ -17,9 +17,9 @@
 //
 // Two forms: single CTAs on tiles of 128 channels x up to 128 rows, and pairs of CTAs (cta_group::2) on 256 x 256, which need two
 // thirds of the copied bytes per product.  The S CTAs (pairs) of a cluster take shares of the k-blocks; at the end each owns
-// every S-th run of four columns, sends its partial sums of the others' runs to their shared memory (st.async, counted by an
-// mbarrier there), and adds what it receives in the order of the shares.  (Read by their owners behind a cluster barrier, the
-// sums took 2500 cycles instead.)
+// a range of columns (runs of four), sends its partial sums of the others' columns to their shared memory, and adds what it
+// receives to its own.  Few columns are sent by the lanes (st.async, counted by an mbarrier at the owner); as that mbarrier counts
+// every 16 bytes apart, 5000 cycles for 256 columns, more than 32 go through shared memory and leave as one bulk copy per owner.
 #include <cuda.h>
 
 #include <cstring>
@@ -35,7 +35,7 @@ int num_sms();
 namespace {
 
 constexpr int kMaxStages = 10;
-constexpr int kThreads = 256;              // warp 0: copies; 1: MMA; all of them: the epilogue
+__host__ __device__ constexpr int threads_of(bool pair) { return pair ? 512 : 256; }      // warp 0: copies; 1: MMA; all: the epilogue
 constexpr size_t kSmemLimit = 226 * 1024;  // of 227 KB, less the control block
 
 struct FpParams {
@@ -50,12 +50,14 @@ struct FpParams {
   int stages;
   uint32_t b_bytes, stage_bytes, tmem_cols, sf_col;
   uint32_t recv_offset;         // of the received sums, in bytes from the ring's start
-  int overlay;                  // they lie in the ring
+  int bulk;                     // sums leave by bulk copies from where the ring was, and are received behind that
+  int max_runs;                 // runs of four columns that a share owns (the last ones fewer)
+  uint32_t owners;              // without bulk copies: the owner of each of up to eight runs, four bits each
   float unit;                   // 2^(sum of the operands' exponents)
   const float* bias;
   int relu;
-  void* y;
-  long long y_stride;
+  uint8_t* y;
+  long long y_pitch;            // bytes
   adaption_stats* stats;
   unsigned long long timeout_ns;
   int stall_at;                 // test aid, see adaption_debug_set
@@ -88,6 +90,16 @@ __device__ __forceinline__ bool fp_wait(uint32_t bar, uint32_t parity, FpCtrl* c
   return fp_wait_slow(bar, parity, ctrl, p, p.timeout_ns, true);
 }
 
+constexpr uint32_t kRunBytes = kRows * 16;
+
+// shared memory of this CTA -> shared memory of a CTA of the cluster, reported to a barrier there
+__device__ __forceinline__ void bulk_copy_to_peer(uint32_t dst_cluster, uint32_t src, uint32_t bytes, uint32_t bar_cluster) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst_cluster),
+               "r"(src), "r"(bytes), "r"(bar_cluster)
+               : "memory");
+}
+// (without the release that would wait for the stores of this thread: the barrier orders uses of shared memory that have ended)
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 // four floats to the shared memory of a CTA of the cluster, counted by a barrier there
 __device__ __forceinline__ void st_async_v4(uint32_t addr, uint32_t bar, int32_t a, int32_t b, int32_t c, int32_t d) {
   asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(addr), "r"(a), "r"(b),
@@ -95,39 +107,11 @@ __device__ __forceinline__ void st_async_v4(uint32_t addr, uint32_t bar, int32_t
                : "memory");
 }
 
-// Four outputs of one channel, `rows` of them real, in rows of y from `at` on; returns how many are stored as 0.
-template <int DT>
-__device__ __forceinline__ uint32_t store_run(const FpParams& p, long long at, const float (&v)[4], int rows) {
-  uint32_t zeros = 0;
-  if (DT == ADAPTION_F32) {
-    float* y = reinterpret_cast<float*>(p.y) + at;
-#pragma unroll
-    for (int k = 0; k < 4; ++k, y += p.y_stride) {
-      if (k < rows) {
-        *y = v[k];
-        zeros += v[k] == 0.f;
-      }
-    }
-  } else {
-    const uint32_t w[2] = {pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3])};
-    uint16_t* y = reinterpret_cast<uint16_t*>(p.y) + at;
-#pragma unroll
-    for (int k = 0; k < 4; ++k, y += p.y_stride) {
-      const uint32_t h = k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu;
-      if (k < rows) {
-        *y = (uint16_t)h;
-        zeros += (h & 0x7fffu) == 0u;
-      }
-    }
-  }
-  return zeros;
-}
-
 template <int BLOCK, bool PAIR, int DT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(threads_of(PAIR), 1)
 fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb, const FpParams p) {
-  constexpr int kGroups = groups_of(BLOCK);
+  constexpr int kGroups = groups_of(BLOCK), kThreads = threads_of(PAIR);
   constexpr uint32_t kSf = (uint32_t)kGroups * kFp4TileBytes;          // scales of a k-block and 128 rows
   extern __shared__ uint8_t smem_raw[];
   __shared__ FpCtrl ctrl;
@@ -166,15 +150,15 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const int to = tile % p.tiles_o, tb = tile / p.tiles_o;
   const int o0 = (PAIR ? to * 2 + (int)half : to) * kRows, b0 = tb * p.BN;
   const int cols = min(p.BN, p.B - b0), col4 = (cols + 3) / 4;         // real columns, in runs of four
-  const int runs = (col4 - share + p.S - 1) / p.S;                     // runs that this CTA finishes: share, share + S, ...
+  const int first_run = share * p.max_runs, runs = max(0, min(p.max_runs, col4 - first_run));     // that this CTA finishes
   const int kb_begin = share * p.kb_per_split;
   const int kb_end = min(p.num_kb, kb_begin + p.kb_per_split);
 
   pdl_wait();
   pdl_launch_dependents();
 
-  // this thread's channel of the epilogue
-  const int my_row = (int)threadIdx.x & (kRows - 1), o = o0 + my_row;
+  // this thread's channel in the epilogue
+  const int o = o0 + ((int)threadIdx.x & (kRows - 1));
   const float bias = p.bias != nullptr && o < p.O ? __ldg(p.bias + o) : 0.f;
 
   bool ok = true;
@@ -236,22 +220,11 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       const uint32_t a = smem_desc_lo(ring) + (uint32_t)s * (p.stage_bytes >> 4), b = a + (kABytes >> 4);
       const uint32_t sf = ((ring + (uint32_t)s * p.stage_bytes + kABytes + p.b_bytes) >> 4) & 0x3FFFu;
       const uint32_t ta = tmem + p.sf_col + (uint32_t)s * slot, tb0 = ta + 4u * kGroups;
-      const bool last = kb == p.num_kb - 1;
-      const int steps = last ? p.steps_last : kBlockElems / kStepElems, groups = last ? p.groups_last : kGroups;
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        if (g < groups) {
-          scales_to_tmem<PAIR>(issue, ta + 4u * g, sf + 32u * g, shi);
-          scales_to_tmem<PAIR>(issue, tb0 + cols_b * g, sf + 32u * (kGroups + g), shi);
-          if (PAIR && p.chunks_b > 1) scales_to_tmem<PAIR>(issue, tb0 + cols_b * g + 4u, sf + 32u * (2 * kGroups + g), shi);
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < kBlockElems / kStepElems; ++k) {
-        const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
-        if (k < steps)
-          mma_fp4<BLOCK, PAIR>(issue, tmem, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g,
-                               tb0 + cols_b * g, (kb > kb_begin || k > 0) ? 1u : 0u);
+      const uint32_t more = kb > kb_begin ? 1u : 0u;
+      if (kb < p.num_kb - 1) {
+        issue_kblock<BLOCK, PAIR>(issue, tmem, a, b, dhi, id, ta, tb0, cols_b, sf, shi, more, kBlockElems / kStepElems, kGroups);
+      } else {
+        issue_kblock<BLOCK, PAIR>(issue, tmem, a, b, dhi, id, ta, tb0, cols_b, sf, shi, more, p.steps_last, p.groups_last);
       }
       if (PAIR) commit_pair_if(issue, smem_u32(&ctrl.empty[s]), mask);
       else tc_commit_if<false>(issue, smem_u32(&ctrl.empty[s]));
@@ -270,82 +243,124 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   }
   __syncwarp();
 
-  // ---- partial sums to their owners: recv[share][run of the owner][128 channels] of 16 bytes
-  if (threadIdx.x == 0 && p.S > 1 && runs > 0) mbar_expect_tx(smem_u32(&ctrl.recv), (uint32_t)(p.S - 1) * (uint32_t)runs * (kRows * 16u));
+  constexpr int kSize = DT == ADAPTION_F32 ? 4 : 2, kParts = kThreads / 128;     // warps per lane quarter: each takes runs of columns in turn
+  const int quarter = warp & 3, part = warp >> 2, row = quarter * 32 + lane;
+  const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16);
+  const bool empty = kb_begin >= kb_end;              // (no k-blocks: the accumulator was never written)
+  ZeroCount<DT> zeros;
   // (warps 2.. wait here for the MMAs, and in a pair the follower's for the leader's)
   ok = fp_wait(smem_u32(&ctrl.done), 0, &ctrl, p) && ok;
   __syncthreads();
-  if (ctas > 1) {
-    if (!PAIR) cluster_wait();                        // (arrived at the start: long complete)
-    if (p.overlay) cluster_sync_all();                // every CTA's ring has come to its end
-  }
-  const uint32_t recv = ring + p.recv_offset, part_bytes = (uint32_t)((col4 + p.S - 1) / p.S) * (kRows * 16u);     // of one share
-  {
-    tc_fence_after();
-    const int quarter = warp & 3, row = quarter * 32 + lane;
-    const uint32_t local = recv + (uint32_t)share * part_bytes + (uint32_t)row * 16u, recv_bar = smem_u32(&ctrl.recv);
-    const bool empty = kb_begin >= kb_end;            // (no k-blocks: the accumulator was never written)
-    for (int c = 16 * (warp >> 2); c < cols; c += 16 * (kThreads / 128)) {
-      int32_t r[2][8];
-      tmem_ld16(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, r[0], r[1]);
-      tmem_ld_wait();
-      pin_after_wait(r[0]);
-      pin_after_wait(r[1]);
-      int owner = (c >> 2) % p.S, place = (c >> 2) / p.S;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (c + 4 * j >= cols) break;
-        int32_t* v = &r[j >> 1][4 * (j & 1)];
-        if (empty) v[0] = v[1] = v[2] = v[3] = 0;
-        const uint32_t at = local + (uint32_t)place * (kRows * 16u);
-        if (owner == share) {
-          st_shared_v4(at, (uint32_t)v[0], (uint32_t)v[1], (uint32_t)v[2], (uint32_t)v[3]);
-        } else {
-          const uint32_t to_rank = PAIR ? 2u * (uint32_t)owner + half : (uint32_t)owner;
-          st_async_v4(mapa_rank(at, to_rank), mapa_rank(recv_bar, to_rank), v[0], v[1], v[2], v[3]);
-        }
-        if (++owner == p.S) { owner = 0; ++place; }
+  tc_fence_after();
+  if (p.S == 1) {
+    // ---- the whole reduction is here: bias, ReLU, store
+    if (!ctrl.abort) {
+      uint8_t* const y = p.y + (long long)b0 * p.y_pitch + (long long)o * kSize;
+      for (int c = 16 * part; c < cols; c += 16 * kParts) {
+        int32_t r[16];
+        tmem_ld16(acc + (uint32_t)c, reinterpret_cast<int32_t(&)[8]>(r[0]), reinterpret_cast<int32_t(&)[8]>(r[8]));
+        tmem_ld_wait();
+        pin_after_wait(reinterpret_cast<int32_t(&)[8]>(r[0]));
+        pin_after_wait(reinterpret_cast<int32_t(&)[8]>(r[8]));
+        if (o < p.O) store_channel<DT, 16>(r, y + (long long)c * p.y_pitch, p.y_pitch, cols - c, p.unit, bias, p.relu != 0, zeros);
       }
     }
-    tc_fence_before();
+  } else {
+    // ---- partial sums to their owners, as runs of four columns: [run][128 channels] of 16 bytes.  Sums of all columns, or of this
+    // CTA's own, lie where the ring was or in the first block of recv; the other shares' blocks follow.
+    if (threadIdx.x == 0 && runs > 0) mbar_expect_tx(smem_u32(&ctrl.recv), (uint32_t)(p.S - 1) * (uint32_t)runs * kRunBytes);
+    if (!PAIR) cluster_wait();                        // (arrived at the start: long complete)
+    if (p.bulk) cluster_arrive_relaxed();             // this CTA's ring has come to its end
+    const uint32_t recv_bar = smem_u32(&ctrl.recv), block_bytes = (uint32_t)p.max_runs * kRunBytes;
+    const uint32_t own = ring + (p.bulk ? (uint32_t)first_run * kRunBytes : p.recv_offset), recv = ring + p.recv_offset + (p.bulk ? 0u : block_bytes);
+    // this CTA's block among another owner's
+    const uint32_t below = recv + (uint32_t)share * block_bytes, above = below - block_bytes;
+#pragma unroll 1
+    for (int c = 16 * part; c < cols; c += 16 * kParts) {
+      int32_t r[16];
+      tmem_ld16(acc + (uint32_t)c, reinterpret_cast<int32_t(&)[8]>(r[0]), reinterpret_cast<int32_t(&)[8]>(r[8]));
+      tmem_ld_wait();
+      pin_after_wait(reinterpret_cast<int32_t(&)[8]>(r[0]));
+      pin_after_wait(reinterpret_cast<int32_t(&)[8]>(r[8]));
+      if (empty) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) r[j] = 0;
+      }
+      if (p.bulk) {
+        // (columns behind the last real one are staged too, up to the tile's width, and never sent or read)
+        const uint32_t at = ring + (uint32_t)(c >> 2) * kRunBytes + (uint32_t)row * 16u;
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+          st_shared_v4(at + (uint32_t)(j >> 2) * kRunBytes, (uint32_t)r[j], (uint32_t)r[j + 1], (uint32_t)r[j + 2], (uint32_t)r[j + 3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          const int run = (c + j) >> 2, owner = (int)(p.owners >> (4 * run)) & 15;
+          if (c + j >= cols) break;
+          const uint32_t at = (uint32_t)(run - owner * p.max_runs) * kRunBytes + (uint32_t)row * 16u;
+          if (owner == share) {
+            st_shared_v4(own + at, (uint32_t)r[j], (uint32_t)r[j + 1], (uint32_t)r[j + 2], (uint32_t)r[j + 3]);
+          } else {
+            const uint32_t to_rank = PAIR ? 2u * (uint32_t)owner + half : (uint32_t)owner;
+            st_async_v4(mapa_rank((share > owner ? above : below) + at, to_rank), mapa_rank(recv_bar, to_rank), r[j], r[j + 1], r[j + 2], r[j + 3]);
+          }
+        }
+      }
+    }
+    if (p.bulk) fence_async_shared();
+    __syncthreads();
+    if (p.bulk) {
+      cluster_wait();                                 // ... and so have the others'
+      // (a copy per run: one for all of an owner's moved 17 bytes a cycle)
+      const int run = (int)threadIdx.x, to = run / p.max_runs;
+      if (run < col4 && to != share) {
+        const uint32_t to_rank = PAIR ? 2u * (uint32_t)to + half : (uint32_t)to;
+        bulk_copy_to_peer(mapa_rank((share > to ? above : below) + (uint32_t)(run - to * p.max_runs) * kRunBytes, to_rank),
+                          ring + (uint32_t)run * kRunBytes, kRunBytes, mapa_rank(recv_bar, to_rank));
+      }
+      __syncwarp();
+    }
+    // Every CTA of the cluster sends, also one that gave up (within its waits' limits), so this wait ends, and no CTA leaves while
+    // sums for it are under way.
+    if (runs > 0 && !mbar_try_wait(recv_bar, 0))
+      ok = fp_wait_slow(recv_bar, 0, &ctrl, p, 4ull * p.timeout_ns + 1000000000ull, false) && ok;
+
+    // ---- the runs this CTA owns: its own sums and the others' in the order of their shares, bias, ReLU, store
+    if (ok && o < p.O && !ctrl.abort) {
+      const uint8_t* const base = smem_raw - smem_u32(smem_raw);
+      const uint32_t offset = (uint32_t)part * kRunBytes + (uint32_t)row * 16u;
+      const uint8_t *mine = base + own + offset, *from = base + recv + offset;
+      int c = 4 * (first_run + part);
+      uint8_t* y = p.y + (long long)(b0 + c) * p.y_pitch + (long long)o * kSize;
+#pragma unroll 2
+      for (int i = part; i < runs; i += kParts) {
+        float4 v = *reinterpret_cast<const float4*>(mine);
+        const uint8_t* next = from;
+#pragma unroll 1
+        for (int k = 1; k < p.S; ++k, next += block_bytes) {
+          const float4 t = *reinterpret_cast<const float4*>(next);
+          v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
+        }
+        const int32_t r[4] = {__float_as_int(v.x), __float_as_int(v.y), __float_as_int(v.z), __float_as_int(v.w)};
+        if (cols - c >= 4) store_channel<DT, 4>(r, y, p.y_pitch, 4, p.unit, bias, p.relu != 0, zeros);
+        else store_channel<DT, 4>(r, y, p.y_pitch, cols - c, p.unit, bias, p.relu != 0, zeros);
+        mine += kParts * kRunBytes;
+        from += kParts * kRunBytes;
+        c += 4 * kParts;
+        y += (long long)(4 * kParts) * p.y_pitch;
+      }
+    }
   }
+  tc_fence_before();
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc<PAIR>(tmem, p.tmem_cols);
   }
-  // Every CTA of the cluster sends, also one that gave up (within its waits' limits), so this wait ends, and no CTA leaves while
-  // sums for it are under way.
-  if (p.S > 1 && runs > 0 && !mbar_try_wait(smem_u32(&ctrl.recv), 0))
-    ok = fp_wait_slow(smem_u32(&ctrl.recv), 0, &ctrl, p, 4ull * p.timeout_ns + 1000000000ull, false) && ok;
-
-  // ---- the runs this CTA owns: sum over the shares, bias, ReLU, store
-  uint32_t zeros = 0;
-  if (ok && o < p.O && !ctrl.abort) {
-    for (int i = (int)threadIdx.x / kRows; i < runs; i += kThreads / kRows) {
-      const uint32_t at = recv + (uint32_t)i * (kRows * 16u) + (uint32_t)my_row * 16u;
-      float4 part[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (k < p.S) part[k] = ld_shared_f4(at + (uint32_t)k * part_bytes);
-      float v[4] = {part[0].x, part[0].y, part[0].z, part[0].w};
-#pragma unroll
-      for (int k = 1; k < 8; ++k)
-        if (k < p.S) { v[0] += part[k].x; v[1] += part[k].y; v[2] += part[k].z; v[3] += part[k].w; }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[k] = fmaf(v[k], p.unit, bias);
-        if (p.relu) v[k] = v[k] < 0.f ? 0.f : v[k];
-      }
-      const int c = 4 * (share + i * p.S);
-      zeros += store_run<DT>(p, (long long)(b0 + c) * p.y_stride + o, v, cols - c);
-    }
-  }
-  __syncwarp();
-  zeros = __reduce_add_sync(0xffffffffu, zeros);
-  if (lane == 0 && zeros) atomicAdd((unsigned long long*)&p.stats->zeros, (unsigned long long)zeros);
-  // (a pair frees TMEM together: neither leaves before the other is that far)
-  if (PAIR) cluster_sync_all();
+  const uint32_t counted = __reduce_add_sync(0xffffffffu, zeros.total());
+  if (lane == 0 && counted) atomicAdd((unsigned long long*)&p.stats->zeros, (unsigned long long)counted);
+  // (a pair frees TMEM together, and what a bulk copy reads stays until it has arrived)
+  if (PAIR || (p.bulk && ctas > 1)) cluster_sync_all();
 }
 
 template <int BLOCK, bool PAIR, int DT>
@@ -361,7 +376,7 @@ int launch_cluster(const CUtensorMap* maps, const FpParams& p, int grid, size_t 
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads_of(PAIR));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -411,7 +426,7 @@ int max_clusters(int ctas) {
   int n = 0;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads_of(true));
   cfg.dynamicSmemBytes = kSmemLimit;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -501,13 +516,14 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   p.b_bytes = (uint32_t)b_rows * kBlockBytes;
   p.stage_bytes = kABytes + p.b_bytes + (uint32_t)(kgroups * kFp4TileBytes * (1 + p.chunks_b));
   const int col4 = ((p.BN < p.B ? p.BN : p.B) + 3) / 4;
-  const size_t sums = (size_t)((col4 + p.S - 1) / p.S) * p.S * 16 * kRows;            // of all shares, for one owner
+  p.max_runs = (col4 + p.S - 1) / p.S;
+  p.bulk = p.S > 1 && col4 > 8 ? 1 : 0;
+  for (int r = 0; r < 8 && r < col4; ++r) p.owners |= (uint32_t)(r / p.max_runs) << (4 * r);
+  // sums that a CTA receives, behind its own
+  const size_t received = p.S > 1 ? (size_t)(p.bulk ? p.S - 1 : p.S) * p.max_runs * kRunBytes : 0;
   p.sf_col = (uint32_t)(p.BN + 31) / 32 * 32;
   const uint32_t slot = (uint32_t)kgroups * 4u * (uint32_t)(1 + p.chunks_b);
-  // the ring has a place of its own beside the sums unless that leaves it too short
-  p.overlay = 2 * sums > kSmemLimit ? 1 : 0;
-  const size_t room = kSmemLimit - 1024 - (p.overlay ? 0 : sums);
-  int stages = (int)(room / p.stage_bytes);
+  int stages = (int)((kSmemLimit - 1024 - (p.bulk ? 0 : received)) / p.stage_bytes);
   if (stages > kMaxStages) stages = kMaxStages;
   if (stages > p.kb_per_split) stages = p.kb_per_split;
   while (stages > 1 && p.sf_col + (uint32_t)stages * slot > 512u) --stages;
@@ -515,15 +531,20 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   p.tmem_cols = 32;
   while (p.tmem_cols < p.sf_col + (uint32_t)stages * slot) p.tmem_cols *= 2;
   size_t smem = (size_t)stages * p.stage_bytes;
-  p.recv_offset = p.overlay ? 0u : (uint32_t)smem;
-  if (!p.overlay) smem += sums;
-  else if (smem < sums) smem = sums;
+  if (p.bulk) {
+    const size_t sums = (size_t)p.BN / 4 * kRunBytes;       // of all columns, where the ring was
+    p.recv_offset = (uint32_t)sums;
+    if (smem < sums + received) smem = sums + received;
+  } else {
+    p.recv_offset = (uint32_t)smem;
+    smem += received;
+  }
   smem += 1024;
   p.unit = pow2_float(g.x.exp + g.w.exp);
   p.bias = g.bias;
   p.relu = g.relu ? 1 : 0;
-  p.y = g.y.data;
-  p.y_stride = g.y.stride;
+  p.y = (uint8_t*)g.y.data;
+  p.y_pitch = g.y.stride * dtype_size(g.y.dtype);
   p.stats = g.stats;
   p.timeout_ns = wait_limit_ns();
   p.stall_at = knob(kStallAt);

@@ -51,11 +51,6 @@ __device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.w
 __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
-}
 // Arrival in the CTAs of `mask` once every instruction issued so far for the pair has retired.
 __device__ __forceinline__ void commit_pair_if(uint32_t issue, uint32_t bar, uint16_t mask) {
   asm volatile(
@@ -125,6 +120,92 @@ __device__ __forceinline__ uint32_t make_idesc_fp4(int block, int n, int m) {
 // ... which two of the four scales of a TMEM word an instruction takes (blocks of 32): bytes 2 * half on
 __device__ __forceinline__ uint32_t scale_half(uint32_t half) { return (half * 2u) << 4 | (half * 2u) << 29; }
 
+
+// Scales to TMEM and MMAs of one k-block: `steps` instructions, `groups` scale tiles per 128 rows.  Scales of A go to the columns from
+// ta on, of B from tb on, cols_b (4 or 8) per tile; in shared memory (from sf, in 16-byte units) those of A come first.
+template <int BLOCK, bool PAIR>
+__device__ __forceinline__ void issue_kblock(uint32_t issue, uint32_t d, uint32_t a, uint32_t b, uint32_t dhi, uint32_t id, uint32_t ta,
+                                             uint32_t tb, uint32_t cols_b, uint32_t sf, uint32_t shi, uint32_t more, int steps, int groups) {
+  constexpr int kGroups = groups_of(BLOCK);
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    if (g < groups) {
+      scales_to_tmem<PAIR>(issue, ta + 4u * g, sf + 32u * g, shi);
+      scales_to_tmem<PAIR>(issue, tb + cols_b * g, sf + 32u * (kGroups + g), shi);
+      if (PAIR && cols_b == 8u) scales_to_tmem<PAIR>(issue, tb + cols_b * g + 4u, sf + 32u * (2 * kGroups + g), shi);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kBlockElems / kStepElems; ++k) {
+    const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
+    if (k < steps)
+      mma_fp4<BLOCK, PAIR>(issue, d, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g, tb + cols_b * g,
+                           k > 0 ? 1u : more);
+  }
+}
+
+// Outputs stored as 0 of one lane: pairs of 16-bit outputs are compared and counted together, in their own type (exact up to 256 pairs).
+template <int DT>
+struct ZeroCount {
+  uint32_t n = 0;
+  __half2 h = __floats2half2_rn(0.f, 0.f);
+  __nv_bfloat162 b = __floats2bfloat162_rn(0.f, 0.f);
+  __device__ __forceinline__ void pair(uint32_t w) {
+    if (DT == ADAPTION_F16) h = __hadd2(h, __heq2(*reinterpret_cast<__half2*>(&w), __floats2half2_rn(0.f, 0.f)));
+    else b = __hadd2(b, __heq2(*reinterpret_cast<__nv_bfloat162*>(&w), __floats2bfloat162_rn(0.f, 0.f)));
+  }
+  __device__ __forceinline__ uint32_t total() const {
+    if (DT == ADAPTION_F32) return n;
+    const float2 f = DT == ADAPTION_F16 ? __half22float2(h) : __bfloat1622float2(b);
+    return n + (uint32_t)(f.x + f.y);
+  }
+};
+template <int DT>
+__device__ __forceinline__ uint32_t relu2(uint32_t w) {       // (a NaN stays one)
+  if (DT == ADAPTION_F16) {
+    const __half2 m = __hmax2_nan(*reinterpret_cast<__half2*>(&w), __floats2half2_rn(0.f, 0.f));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  }
+  const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&w), __floats2bfloat162_rn(0.f, 0.f));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+__device__ __forceinline__ float relu1(float v) {
+  asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v));
+  return v;
+}
+
+// One lane's channel in `N` consecutive batch rows, `rows` of them real (consecutive lanes store consecutive outputs, so that rows of any
+// alignment do).  `at`: the channel in the first row.
+template <int DT, int N>
+__device__ __forceinline__ void store_channel(const int32_t* r, uint8_t* at, long long pitch, int rows, float unit, float bias, bool relu,
+                                              ZeroCount<DT>& zeros) {
+#pragma unroll
+  for (int j = 0; j < N; j += 2) {
+    if (j >= rows) break;
+    float a = fmaf(__int_as_float(r[j]), unit, bias), b = fmaf(__int_as_float(r[j + 1]), unit, bias);
+    uint8_t* const next = at + pitch;
+    if (DT == ADAPTION_F32) {
+      if (relu) { a = relu1(a); b = relu1(b); }
+      zeros.n += a == 0.f;
+      *reinterpret_cast<float*>(at) = a;
+      if (j + 1 < rows) {
+        zeros.n += b == 0.f;
+        *reinterpret_cast<float*>(next) = b;
+      }
+    } else {
+      uint32_t w = pack2<DT>(a, b);
+      if (relu) w = relu2<DT>(w);
+      *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
+      if (j + 1 < rows) {
+        zeros.pair(w);
+        *reinterpret_cast<uint16_t*>(next) = (uint16_t)(w >> 16);
+      } else {
+        zeros.n += (w & 0x7fffu) == 0u;
+      }
+    }
+    at = next + pitch;
+  }
+}
 
 // Codes: boxes of a k-block of `box_rows` rows.  A row ends with its last element's byte: what the box holds behind it arrives as zeros.
 inline bool encode_fp4_codes(CUtensorMap* map, const adaption_fp4tensor& t, int64_t rows, int64_t inner, uint32_t box_rows, bool long_rows) {

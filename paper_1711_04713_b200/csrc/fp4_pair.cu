@@ -91,59 +91,6 @@ __device__ __forceinline__ bool pair_wait(uint32_t bar, uint32_t parity, PairCtr
   return pair_wait_slow(bar, parity, ctrl, p);
 }
 
-// Scales to TMEM and MMAs of one k-block: `steps` instructions, `groups` scale tiles per 128 rows.
-template <int BLOCK>
-__device__ __forceinline__ void issue_kblock(uint32_t issue, uint32_t d, uint32_t a, uint32_t b, uint32_t dhi, uint32_t id, uint32_t ta,
-                                             uint32_t tb, uint32_t sf, uint32_t shi, uint32_t more, int steps, int groups) {
-  constexpr int kGroups = groups_of(BLOCK);
-#pragma unroll
-  for (int g = 0; g < kGroups; ++g) {
-    if (g < groups) {
-      scales_to_tmem<true>(issue, ta + 4u * g, sf + 32u * g, shi);
-      scales_to_tmem<true>(issue, tb + 8u * g, sf + 32u * (kGroups + g), shi);
-      scales_to_tmem<true>(issue, tb + 8u * g + 4u, sf + 32u * (2 * kGroups + g), shi);
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < kBlockElems / kStepElems; ++k) {
-    const uint32_t g = BLOCK == 32 ? (uint32_t)k >> 1 : (uint32_t)k;
-    if (k < steps)
-      mma_fp4<BLOCK, true>(issue, d, a + 2u * k, b + 2u * k, dhi, BLOCK == 32 ? id | scale_half(k & 1) : id, ta + 4u * g, tb + 8u * g,
-                           k > 0 ? 1u : more);
-  }
-}
-
-// Outputs stored as 0 of one lane and tile: pairs of 16-bit outputs are compared and counted together, in their own type (a
-// lane has 64 of them, all counts are exact).
-template <int DT>
-struct ZeroCount {
-  uint32_t n = 0;
-  __half2 h = __floats2half2_rn(0.f, 0.f);
-  __nv_bfloat162 b = __floats2bfloat162_rn(0.f, 0.f);
-  __device__ __forceinline__ void pair(uint32_t w) {
-    if (DT == ADAPTION_F16) h = __hadd2(h, __heq2(*reinterpret_cast<__half2*>(&w), __floats2half2_rn(0.f, 0.f)));
-    else b = __hadd2(b, __heq2(*reinterpret_cast<__nv_bfloat162*>(&w), __floats2bfloat162_rn(0.f, 0.f)));
-  }
-  __device__ __forceinline__ uint32_t total() const {
-    if (DT == ADAPTION_F32) return n;
-    const float2 f = DT == ADAPTION_F16 ? __half22float2(h) : __bfloat1622float2(b);
-    return n + (uint32_t)(f.x + f.y);
-  }
-};
-template <int DT>
-__device__ __forceinline__ uint32_t relu2(uint32_t w) {       // (a NaN stays one)
-  if (DT == ADAPTION_F16) {
-    const __half2 m = __hmax2_nan(*reinterpret_cast<__half2*>(&w), __floats2half2_rn(0.f, 0.f));
-    return *reinterpret_cast<const uint32_t*>(&m);
-  }
-  const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<__nv_bfloat162*>(&w), __floats2bfloat162_rn(0.f, 0.f));
-  return *reinterpret_cast<const uint32_t*>(&m);
-}
-__device__ __forceinline__ float relu1(float v) {
-  asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v));
-  return v;
-}
-
 // Lanes are batch rows, columns are channels: 32 of them from channel `c` on, as half a row (16-bit types: half 0 or 1) or a
 // whole row of the warp's staging block, in the order of the 128-byte swizzle.  The stores from there end on the row's last 16-byte
 // boundary (a store clips at such boundaries only); outputs behind it go to the row `y` at once.
@@ -199,39 +146,6 @@ __device__ __forceinline__ void stage_row(const PairParams& p, const int32_t (&r
           if (e < tail) reinterpret_cast<uint16_t*>(y)[c + i + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
       }
     }
-  }
-}
-
-// Lanes are channels, columns are batch rows: 16 rows from `row` on, this lane's channel of each (consecutive lanes store
-// consecutive outputs, so rows of any alignment do).
-template <int DT>
-__device__ __forceinline__ void finish_channel(const PairParams& p, const int32_t* r, uint8_t* at, int rows, float bias,
-                                               ZeroCount<DT>& zeros) {
-#pragma unroll
-  for (int j = 0; j < 16; j += 2) {
-    if (j >= rows) break;
-    float a = fmaf(__int_as_float(r[j]), p.unit, bias), b = fmaf(__int_as_float(r[j + 1]), p.unit, bias);
-    uint8_t* const next = at + p.y_pitch;
-    if (DT == ADAPTION_F32) {
-      if (p.relu) { a = relu1(a); b = relu1(b); }
-      zeros.n += a == 0.f;
-      *reinterpret_cast<float*>(at) = a;
-      if (j + 1 < rows) {
-        zeros.n += b == 0.f;
-        *reinterpret_cast<float*>(next) = b;
-      }
-    } else {
-      uint32_t w = pack2<DT>(a, b);
-      if (p.relu) w = relu2<DT>(w);
-      *reinterpret_cast<uint16_t*>(at) = (uint16_t)w;
-      if (j + 1 < rows) {
-        zeros.pair(w);
-        *reinterpret_cast<uint16_t*>(next) = (uint16_t)(w >> 16);
-      } else {
-        zeros.n += (w & 0x7fffu) == 0u;
-      }
-    }
-    at = next + p.y_pitch;
   }
 }
 
@@ -348,9 +262,9 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         const bool last = kb == p.num_kb - 1;
         const uint32_t more = kb > 0 ? 1u : 0u;
         if (!last) {
-          issue_kblock<BLOCK>(issue, tmem, a, b, dhi, id, ta, tb, sf, shi, more, kBlockElems / kStepElems, kGroups);
+          issue_kblock<BLOCK, true>(issue, tmem, a, b, dhi, id, ta, tb, 8u, sf, shi, more, kBlockElems / kStepElems, kGroups);
         } else {
-          issue_kblock<BLOCK>(issue, tmem, a, b, dhi, id, ta, tb, sf, shi, more, p.steps_last, p.groups_last);
+          issue_kblock<BLOCK, true>(issue, tmem, a, b, dhi, id, ta, tb, 8u, sf, shi, more, p.steps_last, p.groups_last);
         }
         tc_commit_if<true>(issue, smem_u32(&ctrl.empty[s]));
         s = next_s;
@@ -451,7 +365,8 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         uint8_t* const y = p.y + (long long)col * p.y_pitch + (long long)at * (DT == ADAPTION_F32 ? 4 : 2);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          finish_channel<DT>(p, &r[i >> 1][16 * (i & 1)], y + (long long)(16 * i) * p.y_pitch, p.B - col - 16 * i, bias, zeros);
+          store_channel<DT, 16>(&r[i >> 1][16 * (i & 1)], y + (long long)(16 * i) * p.y_pitch, p.y_pitch, p.B - col - 16 * i, p.unit, bias,
+                                p.relu != 0, zeros);
       }
       counted += zeros.total();
     }
