@@ -536,13 +536,9 @@ int adaption_fp4_act_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_matrix x, 
   if (d_workspace == nullptr || workspace_bytes < adaption_fp4_act_ip_workspace_bytes(B, K, O, w.block))
     return ADAPTION_ERR_WORKSPACE;
   if (!aligned16(d_workspace)) return ADAPTION_ERR_ALIGNMENT;
-  g.x.codes = d_workspace;
-  g.x.scales = static_cast<uint8_t*>(d_workspace) + fp4_codes_bytes(B, K);
-  g.x.c_stride = (K + 31) / 32 * 32;
-  g.x.block = w.block;
-  g.x.exp = x_exp;
-  rc = fp4_quantize_impl(x, nullptr, (size_t)B, (size_t)K, 0, g.x, nullptr, g.stream);
-  return rc != ADAPTION_OK ? rc : fp4_ip_impl(g);
+  g.x_real = x;
+  return fp4_act_ip_impl(g, adaption_fp4tensor{d_workspace, static_cast<uint8_t*>(d_workspace) + fp4_codes_bytes(B, K), (K + 31) / 32 * 32,
+                                               w.block, x_exp});
 }
 
 int adaption_probe_i8_peak(int32_t bn, int32_t pair, int32_t iters, int32_t commit_every, uint64_t* d_cycles,

@@ -33,7 +33,9 @@ int fp4_dequantize_impl(const adaption_fp4tensor& x, size_t outer, size_t inner,
 // y[B][O] = act(x [B][K] w [O][K]^T + bias); arguments checked by the caller
 struct Fp4Problem {
   int64_t B = 0, K = 0, O = 0;
-  adaption_fp4tensor x{}, w{};
+  adaption_fp4tensor x{}, w{};   // x.codes null: the kernel quantizes x_real itself
+  adaption_matrix x_real{};
+  bool x_follows = false;        // x comes from fp4_quantize_impl, the launch right before on the same stream
   const float* bias = nullptr;
   int32_t relu = 0;
   adaption_matrix y{};
@@ -41,6 +43,8 @@ struct Fp4Problem {
   cudaStream_t stream = nullptr;
 };
 int fp4_ip_impl(const Fp4Problem& p);
+// The same on real activations p.x_real; `workspace` describes the place of their 4-bit form.
+int fp4_act_ip_impl(Fp4Problem& p, const adaption_fp4tensor& workspace);
 // The persistent kernel over tiles of 256 channels x 256 rows (csrc/fp4_pair.cu).
 int launch_fp4_pair(const Fp4Problem& p);
 

@@ -15,6 +15,10 @@
 // the MMA reads) into columns that belong to the ring's stage: they are written again only after the MMAs that read
 // them have released the stage.
 //
+// Activations that are still real numbers are quantized into the ring by the warps that are idle in the main loop (FUSED), if they are few:
+// a warp takes a row's 256 elements of a k-block, and the full barrier of a stage counts the rows beside the copies' bytes.
+// That saves a launch; every tile of channels quantizes them anew.
+//
 // Two forms: single CTAs on tiles of 128 channels x up to 128 rows, and pairs of CTAs (cta_group::2) on 256 x 256, which need two
 // thirds of the copied bytes per product.  The S CTAs (pairs) of a cluster take shares of the k-blocks; at the end each owns
 // a range of columns (runs of four), sends its partial sums of the others' columns to their shared memory, and adds what it
@@ -25,6 +29,7 @@
 #include <cstring>
 
 #include "fp4_mma.cuh"
+#include "fp4_quant.cuh"
 #include "knobs.cuh"
 #include "tensor_maps.cuh"
 
@@ -35,7 +40,7 @@ int num_sms();
 namespace {
 
 constexpr int kMaxStages = 10;
-__host__ __device__ constexpr int threads_of(bool pair) { return pair ? 512 : 256; }      // warp 0: copies; 1: MMA; all: the epilogue
+__host__ __device__ constexpr int threads_of(bool pair, bool fused) { return pair || fused ? 512 : 256; }    // warp 0: copies; 1: MMA; all: the epilogue
 constexpr size_t kSmemLimit = 226 * 1024;  // of 227 KB, less the control block
 
 struct FpParams {
@@ -51,6 +56,12 @@ struct FpParams {
   uint32_t b_bytes, stage_bytes, tmem_cols, sf_col;
   uint32_t recv_offset;         // of the received sums, in bytes from the ring's start
   int bulk;                     // sums leave by bulk copies from where the ring was, and are received behind that
+  // FUSED: real activations
+  const uint8_t* x;
+  long long x_pitch;            // bytes
+  int x_aligned, K;             // rows of x lie on 16-byte boundaries
+  float inv_unit, step_unit;    // 2^-exp, 2^exp of their 4-bit form
+  int early;                    // the weights may be read before the kernel in front has ended
   int max_runs;                 // runs of four columns that a share owns (the last ones fewer)
   uint32_t owners;              // without bulk copies: the owner of each of up to eight runs, four bits each
   float unit;                   // 2^(sum of the operands' exponents)
@@ -58,6 +69,7 @@ struct FpParams {
   int relu;
   uint8_t* y;
   long long y_pitch;            // bytes
+  int y_dtype;
   adaption_stats* stats;
   unsigned long long timeout_ns;
   int stall_at;                 // test aid, see adaption_debug_set
@@ -107,11 +119,111 @@ __device__ __forceinline__ void st_async_v4(uint32_t addr, uint32_t bar, int32_t
                : "memory");
 }
 
-template <int BLOCK, bool PAIR, int DT>
-__global__ void __launch_bounds__(threads_of(PAIR), 1)
+template <int DT, int N>
+__device__ __forceinline__ void store_columns(const FpParams& p, const int32_t* r, uint8_t* at, int rows, float bias, uint32_t& zeros) {
+  if (DT >= 0) {
+    ZeroCount<DT> z;
+    store_channel<DT, N>(r, at, p.y_pitch, rows, p.unit, bias, p.relu != 0, z);
+    zeros += z.total();
+  } else if (p.y_dtype == ADAPTION_F32) {
+    store_columns<ADAPTION_F32, N>(p, r, at, rows, bias, zeros);
+  } else if (p.y_dtype == ADAPTION_F16) {
+    store_columns<ADAPTION_F16, N>(p, r, at, rows, bias, zeros);
+  } else {
+    store_columns<ADAPTION_BF16, N>(p, r, at, rows, bias, zeros);
+  }
+}
+
+// Eight elements of a row from element `col` on: as raw words, and as numbers (0 behind the row's end).
+template <int SRC>
+__device__ __forceinline__ void load_eight(const FpParams& p, const uint8_t* row, int col, uint32_t (&w)[8]) {
+  constexpr int kSize = SRC == ADAPTION_F32 ? 4 : 2;
+  const uint8_t* at = row + (long long)col * kSize;
+  if (p.x_aligned && p.K - col >= 8) {
+    const uint4 a = __ldg(reinterpret_cast<const uint4*>(at));
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+    if (SRC == ADAPTION_F32) {
+      const uint4 b = __ldg(reinterpret_cast<const uint4*>(at) + 1);
+      w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+  } else {
+    load_shifted(at, min(p.K - col, 8) * kSize, w);
+  }
+}
+template <int SRC>
+__device__ __forceinline__ float numbers_of(int n, const uint32_t (&w)[8], float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (SRC == ADAPTION_F32) v[k] = __uint_as_float(w[k]);
+    else if (SRC == ADAPTION_F16) v[k] = __half2float(__ushort_as_half((unsigned short)(w[k >> 1] >> (16 * (k & 1)))));
+    else v[k] = __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+  }
+  if (n < 8) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k >= n) v[k] = 0.f;
+  }
+  uint32_t top = 0u;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);    // (magnitudes in order, NaN above them all)
+  return __uint_as_float(top);
+}
+
+// Quantizes the rows b0 .. b0 + rows - 1 of this CTA's k-blocks into the ring's stages; a warp's next item is loaded while it works on
+// one.  No more warps than stages * rows take part: a warp's items are then at most a round of the ring apart, and the wait that it
+// passed for one says that the phase before the one that it waits for next is over (a barrier tells phases apart modulo two only).
+template <int BLOCK, int SRC>
+__device__ __forceinline__ void quantize_into_ring(const FpParams& p, FpCtrl* ctrl, uint32_t ring, int kb_begin, int kb_end, int b0, int rows,
+                                                   int first, int warps, int lane) {
+  constexpr int kLanes = BLOCK / 8;
+  const int blocks = kb_end - kb_begin;
+  if (warps > p.stages * rows) warps = p.stages * rows;
+  if (first >= warps) return;
+  int kb = first / rows, row = first % rows;              // (of this warp's items: first, first + warps, ...)
+  uint32_t w[8];
+  if (kb < blocks) load_eight<SRC>(p, p.x + (long long)(b0 + row) * p.x_pitch, (kb_begin + kb) * kBlockElems + 8 * lane, w);
+  int s = kb, round = 0;                                  // (kb < stages)
+  while (kb < blocks) {
+    const int this_kb = kb, this_row = row, this_s = s, this_round = round;
+    float v[8];
+    const int col = (kb_begin + this_kb) * kBlockElems + 8 * lane;
+    float top = numbers_of<SRC>(p.K - col, w, v);
+    row += warps;
+    while (row >= rows) {
+      row -= rows;
+      ++kb;
+      if (++s == p.stages) { s = 0; ++round; }
+    }
+    if (kb < blocks) load_eight<SRC>(p, p.x + (long long)(b0 + row) * p.x_pitch, (kb_begin + kb) * kBlockElems + 8 * lane, w);
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1)
+      top = __uint_as_float(max(__float_as_uint(top), __shfl_xor_sync(0xffffffffu, __float_as_uint(top), o)));
+    fp4_finite<BLOCK, 8>(v, top);
+    uint32_t code[1];
+    const uint32_t byte = fp4_encode<BLOCK, 8>(v, top, p.inv_unit, p.step_unit, code);
+    __syncwarp();
+    if (this_round > 0 && !__all_sync(0xffffffffu, fp_wait(smem_u32(&ctrl->empty[this_s]), (uint32_t)(this_round - 1) & 1u, ctrl, p))) return;
+    const uint32_t b = ring + (uint32_t)this_s * p.stage_bytes + kABytes;
+    // four bytes of the row, in the order of the 128-byte swizzle
+    const uint32_t at = b + (uint32_t)this_row * 128u + ((((uint32_t)lane >> 2) ^ ((uint32_t)this_row & 7u)) << 4) + ((uint32_t)lane & 3u) * 4u;
+    asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(code[0]) : "memory");
+    if ((lane & (kLanes - 1)) == 0) {
+      const uint32_t j = (uint32_t)lane / kLanes, r = (uint32_t)this_row;
+      const uint32_t sf = b + p.b_bytes + (uint32_t)groups_of(BLOCK) * kFp4TileBytes + (j >> 2) * kFp4TileBytes + (r & 31u) * 16u + (r >> 5) * 4u + (j & 3u);
+      asm volatile("st.shared.b8 [%0], %1;" ::"r"(sf), "r"(byte) : "memory");
+    }
+    fence_async_shared();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&ctrl->full[this_s]));
+  }
+}
+
+// DT: type of y (-1: p.y_dtype).  FUSED: type of the activations that the kernel quantizes itself, -1 where they are 4-bit already.
+template <int BLOCK, bool PAIR, int DT, int FUSED>
+__global__ void __launch_bounds__(threads_of(PAIR, FUSED >= 0), 1)
 fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const __grid_constant__ CUtensorMap map_sfa, const __grid_constant__ CUtensorMap map_sfb, const FpParams p) {
-  constexpr int kGroups = groups_of(BLOCK), kThreads = threads_of(PAIR);
+  constexpr int kGroups = groups_of(BLOCK), kThreads = threads_of(PAIR, FUSED >= 0);
   constexpr uint32_t kSf = (uint32_t)kGroups * kFp4TileBytes;          // scales of a k-block and 128 rows
   extern __shared__ uint8_t smem_raw[];
   __shared__ FpCtrl ctrl;
@@ -122,11 +234,13 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const uint32_t rank = ctas > 1 ? cluster_ctarank() : 0u;
   const int share = (int)(PAIR ? rank >> 1 : rank);                    // of the reduction
   const uint32_t half = PAIR ? rank & 1u : 0u, leader = rank - half;   // place in the pair
-  const int tile = (int)blockIdx.x / ctas;
+  const int tile = (int)blockIdx.x / ctas, to = tile % p.tiles_o, tb = tile / p.tiles_o;
+  const int o0 = (PAIR ? to * 2 + (int)half : to) * kRows, b0 = tb * p.BN;
+  const int cols = min(p.BN, p.B - b0), col4 = (cols + 3) / 4;         // real columns, in runs of four
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      mbar_init(smem_u32(&ctrl.full[s]), 1);
+      mbar_init(smem_u32(&ctrl.full[s]), FUSED >= 0 ? 1 + cols : 1);
       mbar_init(smem_u32(&ctrl.empty[s]), 1);
     }
     mbar_init(smem_u32(&ctrl.done), 1);
@@ -147,12 +261,31 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_after();
   const uint32_t tmem = ctrl.tmem_base;
 
-  const int to = tile % p.tiles_o, tb = tile / p.tiles_o;
-  const int o0 = (PAIR ? to * 2 + (int)half : to) * kRows, b0 = tb * p.BN;
-  const int cols = min(p.BN, p.B - b0), col4 = (cols + 3) / 4;         // real columns, in runs of four
   const int first_run = share * p.max_runs, runs = max(0, min(p.max_runs, col4 - first_run));     // that this CTA finishes
   const int kb_begin = share * p.kb_per_split;
   const int kb_end = min(p.num_kb, kb_begin + p.kb_per_split);
+
+  // Copies of one k-block: operand A (the weights) and operand B, reported to the same barrier.
+  const auto copy_a = [&](int kb, int s) {
+    const uint32_t own = smem_u32(&ctrl.full[s]), dst = ring + (uint32_t)s * p.stage_bytes;
+    if (half == 0u) mbar_expect_tx(own, FUSED >= 0 ? kABytes + kSf : (PAIR ? 2u : 1u) * p.stage_bytes);
+    const uint32_t full = PAIR ? mapa_rank(own, leader) : own;
+    tma_load_2d<PAIR>(dst, &map_a, full, kb * kBlockBytes, o0);
+    tma_load_2d<PAIR>(dst + kABytes + p.b_bytes, &map_sfa, full, kb * kGroups * (kFp4TileBytes / 8), o0 / kRows);
+  };
+  const auto copy_b = [&](int kb, int s) {
+    const uint32_t own = smem_u32(&ctrl.full[s]), dst = ring + (uint32_t)s * p.stage_bytes;
+    const uint32_t full = PAIR ? mapa_rank(own, leader) : own;
+    tma_load_2d<PAIR>(dst + kABytes, &map_b, full, kb * kBlockBytes, PAIR ? b0 + (int)half * (p.BN / 2) : b0);
+    tma_load_2d<PAIR>(dst + kABytes + p.b_bytes + kSf, &map_sfb, full, kb * kGroups * (kFp4TileBytes / 8), b0 / kRows);
+  };
+  // With activations that the kernel before this one quantized, the weights need not wait for it: what wrote them ended before that
+  // kernel passed its own wait, and this one was launched behind that.
+  const int early = p.early ? max(0, min(kb_end - kb_begin, p.stages)) : 0;
+  if (warp == 0 && early > 0 && p.stall_at < 0 && elect_one()) {
+    for (int s = 0; s < early; ++s) copy_a(kb_begin + s, s);
+  }
+  __syncwarp();
 
   pdl_wait();
   pdl_launch_dependents();
@@ -173,14 +306,8 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         if (!ok) break;
       }
       if (issue) {
-        const uint32_t own = smem_u32(&ctrl.full[s]), dst = ring + (uint32_t)s * p.stage_bytes;
-        if (half == 0u) mbar_expect_tx(own, (PAIR ? 2u : 1u) * p.stage_bytes);
-        const uint32_t full = PAIR ? mapa_rank(own, leader) : own;
-        const int words = kb * kGroups * (kFp4TileBytes / 8);
-        tma_load_2d<PAIR>(dst, &map_a, full, kb * kBlockBytes, o0);
-        tma_load_2d<PAIR>(dst + kABytes, &map_b, full, kb * kBlockBytes, PAIR ? b0 + (int)half * (p.BN / 2) : b0);
-        tma_load_2d<PAIR>(dst + kABytes + p.b_bytes, &map_sfa, full, words, o0 / kRows);
-        tma_load_2d<PAIR>(dst + kABytes + p.b_bytes + kSf, &map_sfb, full, words, b0 / kRows);
+        if (issued >= early || p.stall_at >= 0) copy_a(kb, s);
+        if (FUSED < 0) copy_b(kb, s);
       }
       __syncwarp();
       ++issued;
@@ -241,13 +368,15 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       }
     }
   }
+  if (FUSED >= 0 && warp >= 2) quantize_into_ring<BLOCK, FUSED < 0 ? 0 : FUSED>(p, &ctrl, ring, kb_begin, kb_end, b0, cols, warp - 2, kThreads / 32 - 2, lane);
   __syncwarp();
 
-  constexpr int kSize = DT == ADAPTION_F32 ? 4 : 2, kParts = kThreads / 128;     // warps per lane quarter: each takes runs of columns in turn
+  const int size = DT < 0 ? (p.y_dtype == ADAPTION_F32 ? 4 : 2) : (DT == ADAPTION_F32 ? 4 : 2);
+  constexpr int kParts = kThreads / 128;     // warps per lane quarter: each takes runs of columns in turn
   const int quarter = warp & 3, part = warp >> 2, row = quarter * 32 + lane;
   const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16);
   const bool empty = kb_begin >= kb_end;              // (no k-blocks: the accumulator was never written)
-  ZeroCount<DT> zeros;
+  uint32_t zeros = 0;
   // (warps 2.. wait here for the MMAs, and in a pair the follower's for the leader's)
   ok = fp_wait(smem_u32(&ctrl.done), 0, &ctrl, p) && ok;
   __syncthreads();
@@ -255,14 +384,14 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   if (p.S == 1) {
     // ---- the whole reduction is here: bias, ReLU, store
     if (!ctrl.abort) {
-      uint8_t* const y = p.y + (long long)b0 * p.y_pitch + (long long)o * kSize;
+      uint8_t* const y = p.y + (long long)b0 * p.y_pitch + (long long)o * size;
       for (int c = 16 * part; c < cols; c += 16 * kParts) {
         int32_t r[16];
         tmem_ld16(acc + (uint32_t)c, reinterpret_cast<int32_t(&)[8]>(r[0]), reinterpret_cast<int32_t(&)[8]>(r[8]));
         tmem_ld_wait();
         pin_after_wait(reinterpret_cast<int32_t(&)[8]>(r[0]));
         pin_after_wait(reinterpret_cast<int32_t(&)[8]>(r[8]));
-        if (o < p.O) store_channel<DT, 16>(r, y + (long long)c * p.y_pitch, p.y_pitch, cols - c, p.unit, bias, p.relu != 0, zeros);
+        if (o < p.O) store_columns<DT, 16>(p, r, y + (long long)c * p.y_pitch, cols - c, bias, zeros);
       }
     }
   } else {
@@ -331,7 +460,7 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       const uint32_t offset = (uint32_t)part * kRunBytes + (uint32_t)row * 16u;
       const uint8_t *mine = base + own + offset, *from = base + recv + offset;
       int c = 4 * (first_run + part);
-      uint8_t* y = p.y + (long long)(b0 + c) * p.y_pitch + (long long)o * kSize;
+      uint8_t* y = p.y + (long long)(b0 + c) * p.y_pitch + (long long)o * size;
 #pragma unroll 2
       for (int i = part; i < runs; i += kParts) {
         float4 v = *reinterpret_cast<const float4*>(mine);
@@ -342,8 +471,8 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           v.x += t.x; v.y += t.y; v.z += t.z; v.w += t.w;
         }
         const int32_t r[4] = {__float_as_int(v.x), __float_as_int(v.y), __float_as_int(v.z), __float_as_int(v.w)};
-        if (cols - c >= 4) store_channel<DT, 4>(r, y, p.y_pitch, 4, p.unit, bias, p.relu != 0, zeros);
-        else store_channel<DT, 4>(r, y, p.y_pitch, cols - c, p.unit, bias, p.relu != 0, zeros);
+        if (cols - c >= 4) store_columns<DT, 4>(p, r, y, 4, bias, zeros);
+        else store_columns<DT, 4>(p, r, y, cols - c, bias, zeros);
         mine += kParts * kRunBytes;
         from += kParts * kRunBytes;
         c += 4 * kParts;
@@ -357,26 +486,26 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     tc_fence_after();
     tmem_dealloc<PAIR>(tmem, p.tmem_cols);
   }
-  const uint32_t counted = __reduce_add_sync(0xffffffffu, zeros.total());
+  const uint32_t counted = __reduce_add_sync(0xffffffffu, zeros);
   if (lane == 0 && counted) atomicAdd((unsigned long long*)&p.stats->zeros, (unsigned long long)counted);
   // (a pair frees TMEM together, and what a bulk copy reads stays until it has arrived)
   if (PAIR || (p.bulk && ctas > 1)) cluster_sync_all();
 }
 
-template <int BLOCK, bool PAIR, int DT>
+template <int BLOCK, bool PAIR, int DT, int FUSED>
 int launch_cluster(const CUtensorMap* maps, const FpParams& p, int grid, size_t smem, cudaStream_t stream) {
   static std::atomic<uint64_t> prepared{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_failure(e, "fp4_cluster_kernel device");
   if (dev >= 64 || !((prepared.load(std::memory_order_acquire) >> dev) & 1)) {
-    e = cudaFuncSetAttribute(fp4_cluster_kernel<BLOCK, PAIR, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
+    e = cudaFuncSetAttribute(fp4_cluster_kernel<BLOCK, PAIR, DT, FUSED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
     if (e != cudaSuccess) return cuda_failure(e, "fp4_cluster_kernel attribute");
     if (dev < 64) prepared.fetch_or((uint64_t)1 << dev, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(threads_of(PAIR));
+  cfg.blockDim = dim3(threads_of(PAIR, FUSED >= 0));
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -396,7 +525,7 @@ int launch_cluster(const CUtensorMap* maps, const FpParams& p, int grid, size_t 
   cfg.attrs = n ? attr : nullptr;
   cfg.numAttrs = (unsigned)n;
   count_launch();
-  e = cudaLaunchKernelEx(&cfg, fp4_cluster_kernel<BLOCK, PAIR, DT>, maps[0], maps[1], maps[2], maps[3], p);
+  e = cudaLaunchKernelEx(&cfg, fp4_cluster_kernel<BLOCK, PAIR, DT, FUSED>, maps[0], maps[1], maps[2], maps[3], p);
   if (e != cudaSuccess) {
     (void)cudaGetLastError();
     return cuda_failure(e, "fp4_cluster_kernel launch");
@@ -405,20 +534,24 @@ int launch_cluster(const CUtensorMap* maps, const FpParams& p, int grid, size_t 
 }
 
 template <int BLOCK, bool PAIR>
-int launch_cluster(const CUtensorMap* maps, const FpParams& p, int dtype, int grid, size_t smem, cudaStream_t stream) {
-  if (dtype == ADAPTION_F32) return launch_cluster<BLOCK, PAIR, ADAPTION_F32>(maps, p, grid, smem, stream);
-  if (dtype == ADAPTION_F16) return launch_cluster<BLOCK, PAIR, ADAPTION_F16>(maps, p, grid, smem, stream);
-  return launch_cluster<BLOCK, PAIR, ADAPTION_BF16>(maps, p, grid, smem, stream);
+int launch_cluster(const CUtensorMap* maps, const FpParams& p, int grid, size_t smem, cudaStream_t stream) {
+  if (p.y_dtype == ADAPTION_F32) return launch_cluster<BLOCK, PAIR, ADAPTION_F32, -1>(maps, p, grid, smem, stream);
+  if (p.y_dtype == ADAPTION_F16) return launch_cluster<BLOCK, PAIR, ADAPTION_F16, -1>(maps, p, grid, smem, stream);
+  return launch_cluster<BLOCK, PAIR, ADAPTION_BF16, -1>(maps, p, grid, smem, stream);
+}
+template <int BLOCK>
+int launch_fused(const CUtensorMap* maps, const FpParams& p, int x_dtype, int grid, size_t smem, cudaStream_t stream) {
+  if (x_dtype == ADAPTION_F32) return launch_cluster<BLOCK, false, -1, ADAPTION_F32>(maps, p, grid, smem, stream);
+  if (x_dtype == ADAPTION_F16) return launch_cluster<BLOCK, false, -1, ADAPTION_F16>(maps, p, grid, smem, stream);
+  return launch_cluster<BLOCK, false, -1, ADAPTION_BF16>(maps, p, grid, smem, stream);
 }
 
 // Clusters of `ctas` blocks, one block per SM, that the current device runs at a time.  (A cluster stays inside one group of SMs, so
 // there are fewer than SMs / ctas: 74 of 2, 33 of 4, 22 of 6, 15 of 8 on 148 SMs.)  Asked once per device and size.
-int max_clusters(int ctas) {
+int max_clusters(int dev, int sms, int ctas) {
   constexpr int kMaxDevices = 64, kMaxCtas = 8;
   static std::atomic<int> known[kMaxDevices][kMaxCtas + 1];
-  if (ctas == 1) return num_sms();
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return num_sms() / ctas;
+  if (ctas == 1) return sms;
   if (dev < kMaxDevices) {
     const int n = known[dev][ctas].load(std::memory_order_relaxed);
     if (n > 0) return n;
@@ -426,7 +559,7 @@ int max_clusters(int ctas) {
   int n = 0;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(threads_of(true));
+  cfg.blockDim = dim3(threads_of(true, false));
   cfg.dynamicSmemBytes = kSmemLimit;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -434,11 +567,11 @@ int max_clusters(int ctas) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const auto kernel = fp4_cluster_kernel<16, true, ADAPTION_BF16>;
+  const auto kernel = fp4_cluster_kernel<16, true, ADAPTION_BF16, -1>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit) != cudaSuccess ||
       cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
     (void)cudaGetLastError();
-    n = num_sms() / (ctas > 4 ? ctas + 1 : ctas);
+    n = sms / (ctas > 4 ? ctas + 1 : ctas);
     if (n < 1) n = 1;
   }
   if (dev < kMaxDevices) known[dev][ctas].store(n, std::memory_order_relaxed);
@@ -455,6 +588,8 @@ struct FpPlan {
 // 40), a k-block 240 more where nothing hides the issue; 5000 for the first copies, the exchange and the end.
 FpPlan make_plan(const Fp4Problem& g, int only_pair) {
   FpPlan best;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) dev = 64;
   const int sms = num_sms(), kb = (int)((g.K + kBlockElems - 1) / kBlockElems), sf = groups_of(g.w.block) * kFp4TileBytes;
   for (int pair = 0; pair < 2; ++pair) {
     if (only_pair >= 0 && pair != only_pair) continue;
@@ -465,7 +600,7 @@ FpPlan make_plan(const Fp4Problem& g, int only_pair) {
     const double mma = 4.0 * (bn > 80 ? (double)bn / 2 : 40.0);
     const double block = bytes / 64 > mma ? bytes / 64 : mma, out = 12.0 * (double)bn;
     for (int S = 1; S * per <= 8 && S <= kb; ++S) {
-      const int64_t at_once = max_clusters(S * per);
+      const int64_t at_once = max_clusters(dev, sms, S * per);
       const double waves = (double)((tiles + at_once - 1) / at_once);
       const double cycles = waves * ((double)((kb + S - 1) / S) * block + 5000.0 + out);
       if (cycles < best.cycles * 0.97) {          // (more shares only where they are worth it)
@@ -491,7 +626,7 @@ FpPlan make_plan(const Fp4Problem& g, int only_pair) {
 }
 
 int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
-  const bool pair = plan.pair;
+  const bool pair = plan.pair, fused = g.x.codes == nullptr;
   const int block = g.w.block, kgroups = groups_of(block);
   FpParams p;
   std::memset(&p, 0, sizeof(p));
@@ -516,6 +651,7 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   p.b_bytes = (uint32_t)b_rows * kBlockBytes;
   p.stage_bytes = kABytes + p.b_bytes + (uint32_t)(kgroups * kFp4TileBytes * (1 + p.chunks_b));
   const int col4 = ((p.BN < p.B ? p.BN : p.B) + 3) / 4;
+  p.early = g.x_follows ? 1 : 0;
   p.max_runs = (col4 + p.S - 1) / p.S;
   p.bulk = p.S > 1 && col4 > 8 ? 1 : 0;
   for (int r = 0; r < 8 && r < col4; ++r) p.owners |= (uint32_t)(r / p.max_runs) << (4 * r);
@@ -545,31 +681,76 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   p.relu = g.relu ? 1 : 0;
   p.y = (uint8_t*)g.y.data;
   p.y_pitch = g.y.stride * dtype_size(g.y.dtype);
+  p.y_dtype = g.y.dtype;
   p.stats = g.stats;
   p.timeout_ns = wait_limit_ns();
   p.stall_at = knob(kStallAt);
   if (!load_tensor_map_encoders()) return ADAPTION_ERR_CUDA;
   CUtensorMap maps[4];
-  if (!encode_fp4_codes(&maps[0], g.w, p.O, g.K, kRows, true) || !encode_fp4_codes(&maps[1], g.x, p.B, g.K, (uint32_t)b_rows, false) ||
-      !encode_fp4_scales(&maps[2], g.w, p.O, groups, 1) || !encode_fp4_scales(&maps[3], g.x, p.B, groups, (uint32_t)p.chunks_b))
-    return ADAPTION_ERR_CUDA;
+  bool ok = encode_fp4_codes(&maps[0], g.w, p.O, g.K, kRows, true) && encode_fp4_scales(&maps[2], g.w, p.O, groups, 1);
+  if (fused) {
+    maps[1] = maps[0];          // (not used)
+    maps[3] = maps[2];
+    p.x = (const uint8_t*)g.x_real.data;
+    p.x_pitch = g.x_real.stride * dtype_size(g.x_real.dtype);
+    p.x_aligned = aligned16(p.x) && (p.x_pitch & 15) == 0;
+    p.K = (int)g.K;
+    p.inv_unit = pow2_float(-g.x.exp);
+    p.step_unit = pow2_float(g.x.exp);
+  } else {
+    ok = ok && encode_fp4_codes(&maps[1], g.x, p.B, g.K, (uint32_t)b_rows, false) && encode_fp4_scales(&maps[3], g.x, p.B, groups, (uint32_t)p.chunks_b);
+  }
+  if (!ok) return ADAPTION_ERR_CUDA;
   const int grid = (int)(tiles * per * p.S);
-  const int dtype = g.y.dtype;
-  if (pair)
-    return block == 32 ? launch_cluster<32, true>(maps, p, dtype, grid, smem, g.stream) : launch_cluster<16, true>(maps, p, dtype, grid, smem, g.stream);
-  return block == 32 ? launch_cluster<32, false>(maps, p, dtype, grid, smem, g.stream) : launch_cluster<16, false>(maps, p, dtype, grid, smem, g.stream);
+  if (fused)
+    return block == 32 ? launch_fused<32>(maps, p, g.x_real.dtype, grid, smem, g.stream) : launch_fused<16>(maps, p, g.x_real.dtype, grid, smem, g.stream);
+  if (pair) return block == 32 ? launch_cluster<32, true>(maps, p, grid, smem, g.stream) : launch_cluster<16, true>(maps, p, grid, smem, g.stream);
+  return block == 32 ? launch_cluster<32, false>(maps, p, grid, smem, g.stream) : launch_cluster<16, false>(maps, p, grid, smem, g.stream);
 }
 
 }  // namespace
 
-int fp4_ip_impl(const Fp4Problem& g) {
+static FpPlan choose_plan(const Fp4Problem& g) {
   // (tests: one cluster per tile of single CTAs or of pairs, or the persistent kernel, wherever the call would run)
   const int pair = knob(kPair);
-  if (pair == 1 && knob(kCluster) != 2) return launch_fp4_pair(g);
-  FpPlan plan = make_plan(g, pair);
+  FpPlan plan;
+  if (pair == 1 && knob(kCluster) != 2) {
+    plan.persistent = true;
+    return plan;
+  }
+  plan = make_plan(g, pair);
   const int shares = knob(kClusterSize) / (plan.pair ? 2 : 1), most = plan.pair ? 4 : 8;
   if (shares > 0) plan.S = shares < most ? shares : most;
+  return plan;
+}
+
+static int run_plan(const Fp4Problem& g, const FpPlan& plan) {
   return plan.persistent ? launch_fp4_pair(g) : launch_fp4_cluster(g, plan);
+}
+
+int fp4_ip_impl(const Fp4Problem& g) { return run_plan(g, choose_plan(g)); }
+
+// Whether the product quantizes the activations itself.  K = 4096, 4096 channels, in a graph: one row 4.8 us against 5.4 with a launch of its
+// own (one by one 5.5 against 8), eight rows 5.2 against 5.5, sixteen 6.2 against 5.7; 25088 to 4096, one row 14.5 against 15.1, sixteen 34
+// against 16.
+static bool quantizes_itself(const Fp4Problem& g, const FpPlan& plan) {
+  const int mode = knob(kFused);
+  if (mode == 0 || plan.persistent || plan.pair) return false;
+  if (mode == 2) return true;
+  return g.B <= 8;
+}
+
+int fp4_act_ip_impl(Fp4Problem& g, const adaption_fp4tensor& workspace) {
+  const FpPlan plan = choose_plan(g);
+  if (quantizes_itself(g, plan)) {
+    g.x = workspace;
+    g.x.codes = nullptr;
+    return launch_fp4_cluster(g, plan);
+  }
+  g.x = workspace;
+  g.x_follows = true;
+  const int rc = fp4_quantize_impl(g.x_real, nullptr, (size_t)g.B, (size_t)g.K, 0, g.x, nullptr, g.stream);
+  return rc != ADAPTION_OK ? rc : run_plan(g, plan);
 }
 
 }  // namespace adaption

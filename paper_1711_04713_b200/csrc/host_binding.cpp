@@ -558,10 +558,11 @@ int fp4tensor(PyObject* o, long long rows, long long cols, long long device, ada
   if (!attr_i64(o, s_outer, &outer) || !attr_i64(o, s_inner, &inner) || !attr_i64(o, s_c_stride, &cs) ||
       !attr_i64(o, s_block, &block) || !attr_i64(o, s_exp, &exp))
     return -1;
-  // (the scale tiles follow from the row length, so a tensor is used at its own)
+  // (the scale tiles follow from the row length, so a tensor is used at its own; codes and scales lie together, Fp4Tensor has
+  // seen to that)
   if (outer < rows || inner != cols) return 0;
-  const int a = attr_lies_on(o, s_codes, device), b = a > 0 ? attr_lies_on(o, s_scales, device) : a;
-  if (b <= 0) return b;
+  const int here = attr_lies_on(o, s_codes, device);
+  if (here <= 0) return here;
   f->c_stride = cs;
   f->block = (int32_t)block;
   f->exp = exp < -1000 || exp > 1000 ? 1000 : (int32_t)exp;

@@ -282,8 +282,11 @@ def test_inner_product_of_more_tiles_than_the_gpu_has_pairs(block):
         assert s.status == 0 and s.zeros == int((y == 0).sum())
 
 
+@pytest.mark.parametrize("fused", [0, 1, 2])
 @pytest.mark.parametrize("block", [16, 32])
-def test_product_of_real_activations(block):
+def test_product_of_real_activations(block, fused):
+    """Activations quantized in a launch of their own, or by the product where it chooses to, or wherever it can."""
+    B.adaption_debug_set("fused", fused)
     for Bn, K, O, dtype, pad, shift in ((1, 4096, 300, "bf16", 0, 0), (7, 333, 200, "f32", 2, 1), (64, 1024, 256, "f16", 8, 0), (140, 77, 130, "bf16", 1, 0),
                                         (16, 640, 1000, "f32", 0, 0), (17, 8200, 140, "bf16", 0, 0)):
         rng = np.random.default_rng(Bn * K)
@@ -339,6 +342,34 @@ def _layer(Bn, K, O, block, seed):
     q = B.Fp4Tensor.empty(O, K, block, exp)
     B.adaption_fp4_quantize(w, O, K, q)
     return q, dev(rng.normal(0, 0.1, O).astype(np.float32))
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("Bn", [1, 48])
+def test_activations_of_special_values(Bn, block):
+    """NaN counts as 0 and infinities as the largest finite number, in the product as in the quantizer; so do blocks out of E4M3's range."""
+    rng = np.random.default_rng(Bn)
+    x = rng.standard_normal((Bn, 300)).astype(np.float32)
+    x[:, ::37] = np.nan
+    x[0, 64:80] = 0.0
+    x[-1, 100] = np.inf
+    x[-1, 260] = -np.inf
+    x[0, 5] = 1e30
+    x[0, 32:48] *= 1e-30
+    w, wv = operand(rng, 40, 300, block, -2 if block == 16 else 0)
+    exp = -7 if block == 16 else 0
+    code, byte, _ = ms.quantize(x, block, exp)
+    xv = ms.values(code, byte, block, exp)
+    for fused in (0, 2):
+        B.adaption_debug_set("fused", fused)
+        y = torch.empty(Bn, 40, device="cuda")
+        ws = torch.empty(B.fp4_act_ip_workspace_bytes(Bn, 300, 40, block), dtype=torch.uint8, device="cuda")
+        B.adaption_fp4_act_ip_fwd(Bn, 300, 40, dev(x), exp, w, None, False, y, B.new_stats(), ws)
+        got, want = y.double().cpu().numpy(), ms.inner_product(xv, wv)
+        # (sums with the largest finite number may overflow 32 bits)
+        big = np.abs(xv) @ np.abs(wv).T > 1e37
+        check_product(y[~torch.from_numpy(big.any(1))], xv[~big.any(1)], wv, None, False, block, "f32")
+        assert not np.isnan(got[:, :][~big]).any() and want.shape == got.shape
 
 
 @pytest.mark.parametrize("block", [16, 32])
