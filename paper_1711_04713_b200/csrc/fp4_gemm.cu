@@ -580,32 +580,40 @@ int max_clusters(int dev, int sms, int ctas) {
 
 struct FpPlan {
   bool pair = false, persistent = false;
-  int S = 1;
+  int S = 1, BN = 16;
   double cycles = 1e300;
 };
 
-// Estimated cycles, from measured parts: an SM takes 64 bytes of copies a cycle at most, an MMA of N columns N / 2 cycles (at least
-// 40), a k-block 240 more where nothing hides the issue; 5000 for the first copies, the exchange and the end.
+// Estimated cycles.  The form is that of the kernels: a k-block takes the time of its copies (an SM's share of L2's reads) or of its
+// MMAs, no fewer than all operand bytes from HBM; then the sums of the columns are exchanged and stored.  The constants are fitted to 290
+// runs, every number of shares of every form at 19 sizes from 1 to 4096 rows: 11 % off on average, and the choice at most 9 %
+// behind the best one (1 x 25088 -> 4096: 12.1 us with three shares, 12.6 with four; 256 rows of it 18.5, the best 18.4; 128 x 4096 ->
+// 4096 6.9; 512 x 4096 -> 4096 8.6, the best 8.0).
 FpPlan make_plan(const Fp4Problem& g, int only_pair) {
   FpPlan best;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) dev = 64;
   const int sms = num_sms(), kb = (int)((g.K + kBlockElems - 1) / kBlockElems), sf = groups_of(g.w.block) * kFp4TileBytes;
-  for (int pair = 0; pair < 2; ++pair) {
-    if (only_pair >= 0 && pair != only_pair) continue;
-    const int tile_o = pair ? 2 * kRows : kRows, per = pair ? 2 : 1;
-    const int64_t bn = g.B < tile_o ? (g.B + 15) / 16 * 16 : tile_o;
+  for (int form = 0; form < 3; ++form) {
+    // single CTAs; pairs on up to 256 columns, and on 128 of more
+    const bool pair = form > 0;
+    if ((only_pair >= 0 && pair != (only_pair != 0)) || (form == 2 && g.B <= kRows)) continue;
+    const int tile_o = pair ? 2 * kRows : kRows, per = pair ? 2 : 1, most = form == 1 ? 2 * kRows : kRows;
+    const int64_t bn = g.B < most ? (g.B + 15) / 16 * 16 : most;
     const int64_t tiles = ((g.O + tile_o - 1) / tile_o) * ((g.B + bn - 1) / bn);
     const double bytes = (double)kABytes + (double)bn / per * kBlockBytes + (double)sf * (1 + (double)((bn + kRows - 1) / kRows));
-    const double mma = 4.0 * (bn > 80 ? (double)bn / 2 : 40.0);
-    const double block = bytes / 64 > mma ? bytes / 64 : mma, out = 12.0 * (double)bn;
+    const double mma = 4.0 * (bn > 160 ? (double)bn / 2 : 80.0) + 20.0, block = bytes / 60 > mma ? bytes / 60 : mma;
+    const double all = (double)g.K * ((double)g.O + (double)g.B) * (0.5 + 1.0 / g.w.block) / 4500.0;
     for (int S = 1; S * per <= 8 && S <= kb; ++S) {
       const int64_t at_once = max_clusters(dev, sms, S * per);
       const double waves = (double)((tiles + at_once - 1) / at_once);
-      const double cycles = waves * ((double)((kb + S - 1) / S) * block + 5000.0 + out);
-      if (cycles < best.cycles * 0.97) {          // (more shares only where they are worth it)
-        best.pair = pair != 0;
+      const double exchange = (double)bn * (S > 1 ? 3.0 + (65.0 * (S - 1) + 3.0) / S : 24.0) + (pair ? 450.0 : 0.0);
+      const double main_loop = waves * (double)((kb + S - 1) / S) * block;
+      const double cycles = (main_loop > all ? main_loop : all) + waves * (exchange + 4000.0) - 4000.0;      // (a wave's start)
+      if (cycles < best.cycles * 0.98) {
+        best.pair = pair;
         best.S = S;
+        best.BN = (int)bn;
         best.cycles = cycles;
       }
     }
@@ -614,9 +622,7 @@ FpPlan make_plan(const Fp4Problem& g, int only_pair) {
     // the persistent kernel: tiles of 256 x 256 in turn, the stores of all but the last behind the next one's main loop
     const int64_t tiles = ((g.O + 255) / 256) * ((g.B + 255) / 256), pairs = sms / 2;
     const double bytes = 2.0 * kABytes + 3.0 * sf, block = bytes / 64 > 512 ? bytes / 64 : 512;
-    double tile = kb * block + 900.0;
-    if (tile < 4000.0) tile = 4000.0;
-    const double cycles = (double)((tiles + pairs - 1) / pairs) * tile + 8000.0;
+    const double cycles = (double)((tiles + pairs - 1) / pairs) * (kb * block + 4000.0) + 3500.0;
     if (cycles < best.cycles) {
       best.persistent = true;
       best.cycles = cycles;
@@ -632,10 +638,10 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   std::memset(&p, 0, sizeof(p));
   p.O = (int)g.O;
   p.B = (int)g.B;
-  const int tile_o = pair ? 2 * kRows : kRows, most = pair ? 2 * kRows : kRows;
+  const int tile_o = pair ? 2 * kRows : kRows;
   p.tiles_o = (p.O + tile_o - 1) / tile_o;
   // (several column tiles: whole scale tiles each; a pair's half of the columns is a multiple of 8)
-  p.BN = p.B < most ? (p.B + 15) / 16 * 16 : most;
+  p.BN = plan.BN;
   const int64_t tiles = (int64_t)p.tiles_o * ((p.B + p.BN - 1) / p.BN);
   p.chunks_b = (p.BN + kRows - 1) / kRows;
   p.num_kb = (int)((g.K + kBlockElems - 1) / kBlockElems);
@@ -721,6 +727,8 @@ static FpPlan choose_plan(const Fp4Problem& g) {
   plan = make_plan(g, pair);
   const int shares = knob(kClusterSize) / (plan.pair ? 2 : 1), most = plan.pair ? 4 : 8;
   if (shares > 0) plan.S = shares < most ? shares : most;
+  if (knob(kClusterBN) == 128 && plan.pair && g.B > kRows) plan.BN = kRows;
+  if (knob(kClusterBN) == 256 && plan.pair && g.B > kRows) plan.BN = g.B < 2 * kRows ? (int)(g.B + 15) / 16 * 16 : 2 * kRows;
   return plan;
 }
 
