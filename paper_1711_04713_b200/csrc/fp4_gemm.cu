@@ -666,6 +666,12 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   p.sf_col = (uint32_t)(p.BN + 31) / 32 * 32;
   const uint32_t slot = (uint32_t)kgroups * 4u * (uint32_t)(1 + p.chunks_b);
   int stages = (int)((kSmemLimit - 1024 - (p.bulk ? 0 : received)) / p.stage_bytes);
+  // more blocks than SMs: two share one, if that leaves each a ring of three stages
+  const int half = p.bulk ? 0 : (int)((kSmemLimit / 2 - 2048 - received) / p.stage_bytes);
+  if (tiles * per * p.S > num_sms() && half >= 3 && p.sf_col + 3u * slot <= 256u) {
+    stages = half;
+    while (p.sf_col + (uint32_t)stages * slot > 256u) --stages;
+  }
   if (stages > kMaxStages) stages = kMaxStages;
   if (stages > p.kb_per_split) stages = p.kb_per_split;
   while (stages > 1 && p.sf_col + (uint32_t)stages * slot > 512u) --stages;
