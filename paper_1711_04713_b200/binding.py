@@ -162,7 +162,10 @@ def load(path: str | None = None):
     spec = importlib.util.spec_from_file_location("_adaption_native", _build.NATIVE_PATH)
     native = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(native)
-    native.bind(os.path.abspath(path), AdaptionError, *_stream_getters(), torch.float32, torch.float16, torch.bfloat16)
+    samples = (torch.empty(3, 5)[1:, 1:4], torch.empty(4, dtype=torch.bfloat16), torch.empty(2, 3, dtype=torch.float16).t(),
+               torch.empty(0, 4, dtype=torch.uint8), torch.empty(2, 3, 4))
+    native.bind(os.path.abspath(path), AdaptionError, *_stream_getters(), torch.float32, torch.float16, torch.bfloat16,
+                torch.Tensor, getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), samples)
     _native = native
     _lib = lib
     return lib

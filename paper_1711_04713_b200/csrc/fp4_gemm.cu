@@ -585,10 +585,9 @@ struct FpPlan {
 };
 
 // Estimated cycles.  The form is that of the kernels: a k-block takes the time of its copies (an SM's share of L2's reads) or of its
-// MMAs, no fewer than all operand bytes from HBM; then the sums of the columns are exchanged and stored.  The constants are fitted to 290
+// MMAs, all operand bytes come from HBM at 4500 bytes a cycle at most, or 40 per SM at work; then the sums of the columns are exchanged and stored.  The constants are fitted to 290
 // runs, every number of shares of every form at 19 sizes from 1 to 4096 rows: 11 % off on average, and the choice at most 9 %
-// behind the best one (1 x 25088 -> 4096: 12.1 us with three shares, 12.6 with four; 256 rows of it 18.5, the best 18.4; 128 x 4096 ->
-// 4096 6.9; 512 x 4096 -> 4096 8.6, the best 8.0).
+// behind the best one (256 x 25088 -> 4096 18.5 us, the best 18.4; 512 x 4096 -> 4096 8.6, the best 8.0; 777 x 1411 -> 2049 6.8).
 FpPlan make_plan(const Fp4Problem& g, int only_pair) {
   FpPlan best;
   int dev = 0;
@@ -603,14 +602,15 @@ FpPlan make_plan(const Fp4Problem& g, int only_pair) {
     const int64_t tiles = ((g.O + tile_o - 1) / tile_o) * ((g.B + bn - 1) / bn);
     const double bytes = (double)kABytes + (double)bn / per * kBlockBytes + (double)sf * (1 + (double)((bn + kRows - 1) / kRows));
     const double mma = 4.0 * (bn > 160 ? (double)bn / 2 : 80.0) + 20.0, block = bytes / 60 > mma ? bytes / 60 : mma;
-    const double all = (double)g.K * ((double)g.O + (double)g.B) * (0.5 + 1.0 / g.w.block) / 4500.0;
+    const double operands = (double)g.K * ((double)g.O + (double)g.B) * (0.5 + 1.0 / g.w.block);
     for (int S = 1; S * per <= 8 && S <= kb; ++S) {
       const int64_t at_once = max_clusters(dev, sms, S * per);
       const double waves = (double)((tiles + at_once - 1) / at_once);
       const double exchange = (double)bn * (S > 1 ? 3.0 + (65.0 * (S - 1) + 3.0) / S : 24.0) + (pair ? 450.0 : 0.0);
+      const double ctas = (double)(tiles < at_once ? tiles : at_once) * S * per, all = operands / (ctas * 40.0 < 4500.0 ? ctas * 40.0 : 4500.0);
       const double main_loop = waves * (double)((kb + S - 1) / S) * block;
       const double cycles = (main_loop > all ? main_loop : all) + waves * (exchange + 4000.0) - 4000.0;      // (a wave's start)
-      if (cycles < best.cycles * 0.98) {
+      if (cycles < best.cycles) {
         best.pair = pair;
         best.S = S;
         best.BN = (int)bn;
