@@ -90,9 +90,8 @@ __device__ __forceinline__ uint32_t e4m3_nearest(float v) {
   return r & 0xffu;
 }
 __device__ __forceinline__ float e4m3_value(uint32_t byte) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)byte));
-  return __low2float(*reinterpret_cast<__half2*>(&r));
+  // exponent and mantissa in their places of a float are 2^-120 of the value, a denormal one too
+  return __uint_as_float(byte << 20) * 1.329227995784916e36f;
 }
 // E8M0: 2^(byte - 127); 2^-127 is a denormal float, 255 is NaN
 __device__ __forceinline__ float e8m0_value(uint32_t byte) {

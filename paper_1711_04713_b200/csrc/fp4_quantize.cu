@@ -24,8 +24,9 @@ int check_matrix(const adaption_matrix& m, int64_t inner) {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kAhead = 2;            // chunks of a thread whose loads are in flight together
+constexpr int kThreads = 128;        // of the quantizer (with 256 and 62 % of the warps 200704 x 256 fp32 took 38.2 us instead of 35.3)
+constexpr int kValueThreads = 256;
+constexpr int kAhead = 2;            // chunks of a thread whose loads are in flight together, where rows are aligned
 
 enum Source { kF32 = ADAPTION_F32, kF16 = ADAPTION_F16, kBF16 = ADAPTION_BF16, kPlanes = 3 };
 
@@ -207,16 +208,16 @@ __device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, 
 }
 
 template <int SRC, int BLOCK, bool ALIGNED>
-__global__ void __launch_bounds__(kThreads) fp4_quantize_kernel(const QuantParams p) {
+__global__ void __launch_bounds__(kThreads, SRC == kF32 ? 12 : 10) fp4_quantize_kernel(const QuantParams p) {
   pdl_prologue();
-  constexpr int kVec = chunk_of(SRC);
+  constexpr int kVec = chunk_of(SRC), kChunks = ALIGNED ? kAhead : 1;
   Counts cnt;
-  uint32_t w[kAhead][8], row[kAhead];
-  int col[kAhead];
-  bool real[kAhead];
-  const uint32_t base = blockIdx.x * (kThreads * kAhead) + threadIdx.x;
+  uint32_t w[kChunks][8], row[kChunks];
+  int col[kChunks];
+  bool real[kChunks];
+  const uint32_t base = blockIdx.x * (kThreads * kChunks) + threadIdx.x;
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u) {
+  for (int u = 0; u < kChunks; ++u) {
     const uint32_t t = base + u * kThreads;
     real[u] = t < p.total;
     row[u] = real[u] ? divide(t, p.chunks) : 0u;
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(kThreads) fp4_quantize_kernel(const QuantParam
     load_chunk<SRC, ALIGNED>(p, row[u], col[u], real[u] ? p.inner - col[u] : 0, w[u]);
   }
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u)
+  for (int u = 0; u < kChunks; ++u)
     quantize_chunk<SRC, BLOCK>(p, real[u], row[u], col[u], real[u] ? p.inner - col[u] : 0, w[u], cnt);
   if (p.stats != nullptr) flush_counts_block(cnt, p.stats);
 }
@@ -243,6 +244,16 @@ struct ValueParams {
   int64_t pitch;                // of a row of y, in bytes
 };
 
+__device__ __forceinline__ void store_words(void* to, bool aligned32, const uint32_t (&w)[8]) {
+  if (aligned32) {
+    asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    __stcs(reinterpret_cast<uint4*>(to), make_uint4(w[0], w[1], w[2], w[3]));
+    __stcs(reinterpret_cast<uint4*>(to) + 1, make_uint4(w[4], w[5], w[6], w[7]));
+  }
+}
 template <int BLOCK>
 __device__ __forceinline__ float step_of(const ValueParams& p, uint32_t byte) {
   return BLOCK == 32 ? e8m0_value(byte) : e4m3_value(byte) * p.unit;
@@ -250,15 +261,15 @@ __device__ __forceinline__ float step_of(const ValueParams& p, uint32_t byte) {
 
 // Rows of y on 16-byte boundaries: a lane takes a chunk of codes, which lies in one block.
 template <int DT, int BLOCK>
-__global__ void __launch_bounds__(kThreads) fp4_values_kernel(const ValueParams p) {
+__global__ void __launch_bounds__(kValueThreads) fp4_values_kernel(const ValueParams p) {
   pdl_prologue();
   constexpr int kVec = chunk_of(DT);
   uint32_t code[kAhead][kVec / 8], byte[kAhead], row[kAhead];
   int col[kAhead];
-  const uint32_t base = blockIdx.x * (kThreads * kAhead) + threadIdx.x;
+  const uint32_t base = blockIdx.x * (kValueThreads * kAhead) + threadIdx.x;
 #pragma unroll
   for (int u = 0; u < kAhead; ++u) {
-    const uint32_t t = base + u * kThreads;
+    const uint32_t t = base + u * kValueThreads;
     row[u] = t < p.total ? divide(t, p.chunks) : 0u;
     col[u] = t < p.total ? (int)(t - row[u] * p.chunks.d) * kVec : p.inner;
     if (col[u] < p.inner) {
@@ -291,14 +302,7 @@ __global__ void __launch_bounds__(kThreads) fp4_values_kernel(const ValueParams 
     }
     uint8_t* to = p.y + (int64_t)row[u] * p.pitch + (int64_t)col[u] * (DT == kF32 ? 4 : 2);
     if (n >= kVec) {
-      if (p.aligned32) {
-        asm volatile("st.global.cs.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                     "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                     : "memory");
-      } else {
-        __stcs(reinterpret_cast<uint4*>(to), make_uint4(w[0], w[1], w[2], w[3]));
-        __stcs(reinterpret_cast<uint4*>(to) + 1, make_uint4(w[4], w[5], w[6], w[7]));
-      }
+      store_words(to, p.aligned32 != 0, w);
     } else {
 #pragma unroll
       for (int k = 0; k < kVec; ++k) {
@@ -311,67 +315,57 @@ __global__ void __launch_bounds__(kThreads) fp4_values_kernel(const ValueParams 
 }
 
 // Rows of y anywhere: a lane takes an aligned 32-byte piece of y, whose elements start anywhere in a byte of codes and in a
-// block.  `chunks` counts the pieces that a row can touch.
+// block.  `chunks` counts the pieces that a row can touch.  (One piece a lane: two in flight took 18.3 us for 4093 x 4099 fp32
+// instead of 16.8.)
 template <int DT, int BLOCK>
-__global__ void __launch_bounds__(kThreads) fp4_values_shifted_kernel(const ValueParams p) {
+__global__ void __launch_bounds__(kValueThreads) fp4_values_shifted_kernel(const ValueParams p) {
   pdl_prologue();
   constexpr int kVec = chunk_of(DT), kSize = 32 / kVec, kWords = kVec / 8;
-  uint32_t code[kAhead][kWords + 1], byte0[kAhead], byte1[kAhead];
-  int c0[kAhead], c1[kAhead];              // first and last element of the piece that exist
-  uint8_t* to[kAhead];
+  const uint32_t t = blockIdx.x * kValueThreads + threadIdx.x;
+  if (t >= p.total) return;
+  const uint32_t row = divide(t, p.chunks);
+  uint8_t* const y = p.y + (int64_t)row * p.pitch;
+  const int off = (int)(reinterpret_cast<uintptr_t>(y) & 31u) / kSize;
+  const int col = (int)(t - row * p.chunks.d) * kVec - off;         // negative: the piece begins before the row
+  const int c0 = max(col, 0), c1 = min(col + kVec, p.inner) - 1;    // first and last element of the piece that exist
+  if (c0 > c1) return;
+  const uint32_t* const codes = reinterpret_cast<const uint32_t*>(p.codes + (int64_t)row * p.row_bytes) + (c0 >> 3);
+  const int more = (c1 >> 3) - (c0 >> 3);
+  uint32_t code[kWords + 1];
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u) {
-    const uint32_t t = blockIdx.x * (kThreads * kAhead) + u * kThreads + threadIdx.x;
-    const uint32_t row = t < p.total ? divide(t, p.chunks) : 0u;
-    uint8_t* const y = p.y + (int64_t)row * p.pitch;
-    const int off = (int)(reinterpret_cast<uintptr_t>(y) & 31u) / kSize;
-    const int col = (int)(t - row * p.chunks.d) * kVec - off;         // negative: the piece begins before the row
-    c0[u] = max(col, 0);
-    c1[u] = t < p.total ? min(col + kVec, p.inner) - 1 : -1;
-    to[u] = y + (int64_t)c0[u] * kSize;
-    if (c0[u] <= c1[u]) {
-      const uint32_t* const codes = reinterpret_cast<const uint32_t*>(p.codes + (int64_t)row * p.row_bytes);
-      const int first = c0[u] >> 3, last = c1[u] >> 3;
+  for (int i = 0; i <= kWords; ++i) code[i] = i <= more ? __ldg(codes + i) : 0u;
+  const int j0 = c0 / BLOCK, j1 = c1 / BLOCK;
+  const uint32_t byte0 = __ldg(p.scales + fp4_scale_offset(row, j0, p.groups));
+  const uint32_t byte1 = j1 == j0 ? byte0 : __ldg(p.scales + fp4_scale_offset(row, j1, p.groups));
+  const float s0 = step_of<BLOCK>(p, byte0), s1 = step_of<BLOCK>(p, byte1);
+  const int border = j1 * BLOCK - c0;                               // elements from here on lie in the second block
+  uint32_t w[8];
 #pragma unroll
-      for (int i = 0; i <= kWords; ++i) code[u][i] = first + i <= last ? __ldg(codes + first + i) : 0u;
-      const int j0 = c0[u] / BLOCK, j1 = c1[u] / BLOCK;
-      byte0[u] = __ldg(p.scales + fp4_scale_offset(row, j0, p.groups));
-      byte1[u] = j1 == j0 ? byte0[u] : __ldg(p.scales + fp4_scale_offset(row, j1, p.groups));
+  for (int i = 0; i < kWords; ++i) {
+    const uint32_t eight = __funnelshift_r(code[i], code[i + 1], 4 * (c0 & 7));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = 8 * i + 2 * k;
+      const float2 f = __half22float2(fp4_unpack2((eight >> (8 * k)) & 255u));
+      const float a = f.x * (e < border ? s0 : s1), b = f.y * (e + 1 < border ? s0 : s1);
+      if (DT == kF32) {
+        w[e & 7] = __float_as_uint(a);
+        w[(e + 1) & 7] = __float_as_uint(b);
+      } else {
+        w[e >> 1] = pack2<DT>(a, b);
+      }
     }
   }
+  uint8_t* const to = y + (int64_t)c0 * kSize;
+  const int n = c1 - c0 + 1;
+  if (n == kVec) {
+    store_words(to, true, w);
+  } else {
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u) {
-    const int n = c1[u] - c0[u] + 1;
-    if (n <= 0) continue;
-    const float s0 = step_of<BLOCK>(p, byte0[u]), s1 = step_of<BLOCK>(p, byte1[u]);
-    const int border = c1[u] / BLOCK * BLOCK - c0[u];                 // elements from here on lie in the second block
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) {
-      const uint32_t eight = __funnelshift_r(code[u][i], code[u][i + 1], 4 * (c0[u] & 7));
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int e = 8 * i + 2 * k;
-        const float2 f = __half22float2(fp4_unpack2((eight >> (8 * k)) & 255u));
-        const float a = f.x * (e < border ? s0 : s1), b = f.y * (e + 1 < border ? s0 : s1);
-        if (DT == kF32) {
-          w[e & 7] = __float_as_uint(a);
-          w[(e + 1) & 7] = __float_as_uint(b);
-        } else {
-          w[e >> 1] = pack2<DT>(a, b);
-        }
-      }
-    }
-    if (n == kVec) {
-      __stcs(reinterpret_cast<uint4*>(to[u]), make_uint4(w[0], w[1], w[2], w[3]));
-      __stcs(reinterpret_cast<uint4*>(to[u]) + 1, make_uint4(w[4], w[5], w[6], w[7]));
-    } else {
-#pragma unroll
-      for (int k = 0; k < kVec; ++k) {
-        if (k >= n) break;
-        if (DT == kF32) reinterpret_cast<uint32_t*>(to[u])[k] = w[k & 7];
-        else reinterpret_cast<uint16_t*>(to[u])[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
-      }
+    for (int k = 0; k < kVec; ++k) {
+      if (k >= n) break;
+      if (DT == kF32) reinterpret_cast<uint32_t*>(to)[k] = w[k & 7];
+      else reinterpret_cast<uint16_t*>(to)[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
     }
   }
 }
@@ -380,10 +374,10 @@ unsigned blocks_of(uint32_t total, int per_block) { return (total + (uint32_t)pe
 
 template <int SRC, int BLOCK>
 int launch_quantize(const QuantParams& p, bool aligned, cudaStream_t stream) {
-  const dim3 grid(blocks_of(p.total, kThreads * kAhead)), block(kThreads);
-  return cuda_status(aligned || SRC == kPlanes
-                         ? launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, true>, grid, block, stream, p)
-                         : launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, false>, grid, block, stream, p),
+  aligned = aligned || SRC == kPlanes;
+  const dim3 grid(blocks_of(p.total, kThreads * (aligned ? kAhead : 1))), block(kThreads);
+  return cuda_status(aligned ? launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, true>, grid, block, stream, p)
+                             : launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, false>, grid, block, stream, p),
                      "fp4_quantize_kernel launch");
 }
 template <int SRC>
@@ -393,7 +387,7 @@ int launch_quantize(const QuantParams& p, int block, bool aligned, cudaStream_t 
 
 template <int DT, int BLOCK>
 int launch_values(const ValueParams& p, bool aligned, cudaStream_t stream) {
-  const dim3 grid(blocks_of(p.total, kThreads * kAhead)), block(kThreads);
+  const dim3 grid(blocks_of(p.total, kValueThreads * (aligned ? kAhead : 1))), block(kValueThreads);
   return cuda_status(aligned ? launch_after_predecessor(fp4_values_kernel<DT, BLOCK>, grid, block, stream, p)
                              : launch_after_predecessor(fp4_values_shifted_kernel<DT, BLOCK>, grid, block, stream, p),
                      "fp4_values_kernel launch");
