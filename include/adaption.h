@@ -310,7 +310,7 @@ ADAPTION_API int adaption_choose_frac_bits_from_acc(int64_t max_abs_acc, int32_t
  * of 4 bits (E2M1: bit 3 the sign, bits 0-2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6) and stands for c * step:
  *   block 32: step = 2^(b - 127), b the block's scale byte (E8M0; 255 is NaN and never written);
  *             `exp` has to be 0;
- *   block 16: step = e4m3(b) * 2^exp, b a byte of E4M3 without sign (at most 448) and exp one
+ *   block 16: step = e4m3(b) * 2^exp, b a byte of E4M3 without sign (at most 448; 127 is NaN and never written) and exp one
  *             exponent for the whole tensor, -63 <= exp <= 63 (adaption_fp4_choose_exp).
  * Storage of a tensor of `outer` rows of `inner` elements:
  *   codes    rows of c_stride / 2 bytes, two elements a byte, the even one in bits 0-3; c_stride >= inner is

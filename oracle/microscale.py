@@ -52,7 +52,7 @@ def values(code, byte, block, exp=0):
     if block == 32:
         step = np.where(byte == 255, np.nan, np.ldexp(1.0, byte - 127))
     else:
-        step = np.ldexp(E4M3[byte], exp)
+        step = np.where(byte == 127, np.nan, np.ldexp(E4M3[np.minimum(byte, 126)], exp))
     v = E2M1[code & 7] * np.repeat(step, block, axis=1)[:, :code.shape[1]]
     return np.where(code & 8, -v, v)
 

@@ -688,6 +688,13 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
     smem += received;
   }
   smem += 1024;
+  // CTAs that wait for one another take at least the share of an SM's shared memory that they take of its TMEM, so that what lies beside
+  // them never wants more columns than there are: two clusters (of two streams, say) that each hold columns which a CTA of the other one
+  // waits for would never end.
+  if (per * p.S > 1) {
+    const size_t least = p.tmem_cols > 256 ? kSmemLimit : (p.tmem_cols > 128 ? (size_t)112 * 1024 : (size_t)64 * 1024);
+    if (smem < least) smem = least;
+  }
   p.unit = pow2_float(g.x.exp + g.w.exp);
   p.bias = g.bias;
   p.relu = g.relu ? 1 : 0;

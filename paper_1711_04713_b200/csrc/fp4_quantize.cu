@@ -11,6 +11,7 @@ int check_fp4(const adaption_fp4tensor& t, int64_t inner) {
   if (t.block == 32 ? t.exp != 0 : (t.exp < -63 || t.exp > 63)) return ADAPTION_ERR_INVALID_ARG;
   if (t.codes == nullptr || t.scales == nullptr) return ADAPTION_ERR_INVALID_ARG;
   if (t.c_stride < inner || (t.c_stride & 31) != 0) return ADAPTION_ERR_INVALID_ARG;
+  if (t.c_stride > 2 * kFp4MaxInner) return ADAPTION_ERR_UNSUPPORTED;
   if (!aligned16(t.codes) || !aligned16(t.scales)) return ADAPTION_ERR_ALIGNMENT;
   return ADAPTION_OK;
 }
@@ -256,7 +257,8 @@ __device__ __forceinline__ void store_words(void* to, bool aligned32, const uint
 }
 template <int BLOCK>
 __device__ __forceinline__ float step_of(const ValueParams& p, uint32_t byte) {
-  return BLOCK == 32 ? e8m0_value(byte) : e4m3_value(byte) * p.unit;
+  if (BLOCK == 32) return e8m0_value(byte);
+  return (byte & 127u) == 127u ? __uint_as_float(0x7fc00000u) : e4m3_value(byte & 127u) * p.unit;
 }
 
 // Rows of y on 16-byte boundaries: a lane takes a chunk of codes, which lies in one block.
@@ -412,7 +414,6 @@ int fp4_quantize_impl(const adaption_matrix& x, const adaption_qtensor* q, size_
   if (inner > (size_t)kFp4MaxInner || outer > (size_t)1 << 40) return ADAPTION_ERR_UNSUPPORTED;
   int rc = check_fp4(out, (int64_t)inner);
   if (rc != ADAPTION_OK) return rc;
-  if (out.c_stride > 2 * kFp4MaxInner) return ADAPTION_ERR_UNSUPPORTED;
   rc = q != nullptr ? check_qtensor_in(*q, (int64_t)inner) : check_matrix(x, (int64_t)inner);
   if (rc != ADAPTION_OK) return rc;
   QuantParams p{};

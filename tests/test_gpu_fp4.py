@@ -155,7 +155,7 @@ def test_dequantize(dtype, block):
     for outer, inner, pad, shift, exp, wide in ((1, 1, 0, 0, 0, 0), (16, 256, 0, 0, 0, 0), (130, 77, 3, 0, -9, 0), (3, 1003, 8, 0, 5, 64),
                                                 (257, 40, 0, 1, -3, 0)):
         blocks = -(-inner // block)
-        top = 256 if block == 32 else 127
+        top = 256 if block == 32 else 128
         byte = ((np.arange(outer * blocks) * 7) % top).astype(np.uint8).reshape(outer, blocks)
         code = rng.integers(0, 16, (outer, inner)).astype(np.uint8)
         exp = exp if block == 16 else 0
