@@ -10,16 +10,16 @@ namespace adaption {
 
 constexpr int kFp4TileRows = 128;      // rows of a scale tile
 constexpr int kFp4TileBytes = 512;     // 128 rows x 4 blocks
-constexpr int64_t kFp4MaxInner = (int64_t)1 << 24;   // longest row: 128 of them (pitches up to twice that) are 2^29 chunks of 8
+constexpr int64_t kFp4MaxInner = (int64_t)1 << 24;   // longest row: the codes of 128 of them (pitches up to twice that) are 2^31 bytes
 
 inline int64_t fp4_blocks(int64_t inner, int block) { return (inner + block - 1) / block; }
 // scale tiles of one row of tiles
 inline int64_t fp4_groups(int64_t inner, int block) { return (fp4_blocks(inner, block) + 3) / 4; }
 
-// Offset of the scale byte of row r and block j; `groups` scale tiles per row of tiles.
-__device__ __forceinline__ int64_t fp4_scale_offset(uint32_t r, int j, int groups) {
-  const uint32_t in_tile = (r & 31u) * 16u + ((r >> 5) & 3u) * 4u + ((uint32_t)j & 3u);
-  return (int64_t)((r >> 7) * (uint64_t)(uint32_t)groups + (uint32_t)(j >> 2)) * kFp4TileBytes + in_tile;
+// Offset of the scale byte of row r and block j; `groups` scale tiles per row of tiles.  (Below 2^32: kernels get a part of the rows.)
+__device__ __forceinline__ uint32_t fp4_scale_offset(uint32_t r, int j, int groups) {
+  const uint32_t tile = (r >> 7) * (uint32_t)groups + ((uint32_t)j >> 2);
+  return tile * kFp4TileBytes + (r & 31u) * 16u + ((r >> 5) & 3u) * 4u + ((uint32_t)j & 3u);
 }
 
 int check_fp4(const adaption_fp4tensor& t, int64_t inner);

@@ -39,16 +39,14 @@ struct Divider {
   uint32_t d, mul, shift;
 };
 Divider make_divider(uint32_t d) {
-  // floor(n / d) = (n * mul) >> shift with mul = ceil(2^shift / d), shift = 31 + floor(log2 d): mul * d exceeds 2^shift by
-  // e < d < 2^(shift - 30), so the product is n / d + (n e / 2^shift) / d, less than 1 / d too large
-  uint32_t shift = 31;
-  while ((d >> (shift - 30)) != 0) ++shift;
-  const uint64_t p = (uint64_t)1 << shift;
+  // floor(n / d) = (2 n * mul) >> (32 + shift) with mul = ceil(2^(31 + shift) / d), shift = floor(log2 d): mul * d exceeds 2^(31 + shift) by
+  // e < d < 2^(shift + 1), so the product is n / d + (n e / 2^(31 + shift)) / d, less than 1 / d too large
+  uint32_t shift = 0;
+  while ((d >> (shift + 1)) != 0) ++shift;
+  const uint64_t p = (uint64_t)1 << (31 + shift);
   return Divider{d, (uint32_t)((p + d - 1) / d), shift};
 }
-__device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& v) {
-  return (uint32_t)(((uint64_t)n * v.mul) >> v.shift);
-}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divider& v) { return __umulhi(n + n, v.mul) >> v.shift; }
 
 // Bytes of `a` by selector; one with bit 3 set is eight times the byte's sign.
 __device__ __forceinline__ uint32_t with_signs(uint32_t a, uint32_t selector) {
@@ -65,7 +63,7 @@ struct QuantParams {
   int aligned32;
   uint8_t* codes;
   uint8_t* scales;
-  int64_t row_bytes;            // of the codes
+  uint32_t row_bytes;           // of the codes
   int groups;
   uint32_t total;               // chunks of all rows
   Divider chunks;               // ... of one row
@@ -95,6 +93,12 @@ __device__ __forceinline__ void load_chunk(const QuantParams& p, uint32_t row, i
     load_words(at, p.aligned32 != 0, w);
   else
     load_shifted(at, min(n, kVec) * kSize, w);
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
 
 // Quantizes one chunk; every lane of the warp comes along (n = 0: nothing to quantize, but codes and scales of the padding).
@@ -136,22 +140,20 @@ __device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, 
       v[2 * k + 1] = fmaf(__uint_as_float(__byte_perm(q[k], 0x4b000000u, 0x7632)), p.unit, less);
     }
   } else if (SRC == kF32) {
-    uint32_t m = 0u;
     if (n < kVec) {
 #pragma unroll
       for (int k = 0; k < kVec; ++k)
         if (k >= n) w[k] = 0u;
     }
+    // (relu: what has a sign is negative as a whole number too; a NaN stays one in the maximum)
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
       if (p.relu) w[k] = (uint32_t)max((int32_t)w[k], 0);
-      m = max(m, w[k] & 0x7fffffffu);
+      v[k] = __uint_as_float(w[k]);
+      top = max_nan(top, fabsf(v[k]));
     }
 #pragma unroll
-    for (int o = 1; o < BLOCK / kVec; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-#pragma unroll
-    for (int k = 0; k < kVec; ++k) v[k] = __uint_as_float(w[k]);
-    top = __uint_as_float(m);
+    for (int o = 1; o < BLOCK / kVec; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
   } else {
     // magnitudes as 16-bit numbers, two at a time; relu: what has a sign is negative as a 16-bit number too
     uint32_t m = 0u;
@@ -180,7 +182,7 @@ __device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, 
     }
     top = SRC == kF16 ? __half2float(__ushort_as_half((unsigned short)m)) : __uint_as_float(m << 16);
   }
-  if (SRC != kPlanes) fp4_finite<BLOCK, kVec>(v, top);
+  if (SRC != kPlanes) fp4_finite<BLOCK, kVec>(v, top);      // (a NaN fails its comparison)
   uint32_t code[kVec / 8];
   const uint32_t byte = fp4_encode<BLOCK, kVec>(v, top, p.inv_unit, p.step_unit, code);
   if (p.stats != nullptr) {
@@ -194,7 +196,7 @@ __device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, 
     }
   }
   if (real) {
-    uint8_t* to = p.codes + (int64_t)row * p.row_bytes + (col >> 1);
+    uint8_t* to = p.codes + (row * p.row_bytes + (uint32_t)(col >> 1));
     if (kVec == 16) *reinterpret_cast<uint2*>(to) = make_uint2(code[0], code[kVec / 8 - 1]);
     else *reinterpret_cast<uint32_t*>(to) = code[0];
   }
@@ -399,9 +401,9 @@ int launch_values(const ValueParams& p, int block, bool aligned, cudaStream_t st
   return block == 32 ? launch_values<DT, 32>(p, aligned, stream) : launch_values<DT, 16>(p, aligned, stream);
 }
 
-// Rows per launch: chunks are counted below 2^29.  A multiple of a scale tile's rows.
+// Rows per launch: chunks are counted below 2^27, so that offsets in codes and scales stay below 2^32.  A multiple of a scale tile's rows.
 int64_t rows_per_launch(int64_t chunks) {
-  const int64_t rows = (((int64_t)1 << 29) / chunks) & ~(int64_t)(kFp4TileRows - 1);
+  const int64_t rows = (((int64_t)1 << 27) / chunks) & ~(int64_t)(kFp4TileRows - 1);
   return rows > kFp4TileRows ? rows : kFp4TileRows;
 }
 
@@ -419,7 +421,7 @@ int fp4_quantize_impl(const adaption_matrix& x, const adaption_qtensor* q, size_
   QuantParams p{};
   p.inner = (int)inner;
   p.c_stride = (int)out.c_stride;
-  p.row_bytes = out.c_stride / 2;
+  p.row_bytes = (uint32_t)(out.c_stride / 2);
   p.groups = (int)fp4_groups((int64_t)inner, out.block);
   p.blocks4 = p.groups * 4;
   p.inv_unit = pow2_float(-out.exp);
