@@ -200,7 +200,7 @@ __device__ __forceinline__ void quantize_into_ring(const FpParams& p, FpCtrl* ct
       top = __uint_as_float(max(__float_as_uint(top), __shfl_xor_sync(0xffffffffu, __float_as_uint(top), o)));
     fp4_finite<BLOCK, 8>(v, top);
     uint32_t code[1];
-    const uint32_t byte = fp4_encode<BLOCK, 8>(v, top, p.inv_unit, p.step_unit, code);
+    const uint32_t byte = fp4_encode<BLOCK, 8, SRC != ADAPTION_F32>(v, top, p.inv_unit, p.step_unit, code);
     __syncwarp();
     if (this_round > 0 && !__all_sync(0xffffffffu, fp_wait(smem_u32(&ctrl->empty[this_s]), (uint32_t)(this_round - 1) & 1u, ctrl, p))) return;
     const uint32_t b = ring + (uint32_t)this_s * p.stage_bytes + kABytes;

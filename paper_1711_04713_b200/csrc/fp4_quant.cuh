@@ -12,6 +12,9 @@
 //     to one unit in the last place (Markstein, IBM J. Res. Dev. 34, 1990): the residual is exact in one fused multiply-add, the
 //     correction leaves an error of 2^-44 before the last rounding, and an element costs three operations.  The same holds
 //     for amax / 6 against the borders of E4M3.
+//     Sources of 16 bits need two: an x off a border is off by 2^-16 of it at least.  With r raised by four units in the last place
+//     the product lies above x / step by 2^-24 to 2^-20 of it; cut to 20 bits it is m on the border m, and stays on its side
+//     of every other.  (4096 x 25088 bf16 in blocks of 16: 46.1 us instead of 46.8.)
 #pragma once
 
 #include "fp4.cuh"
@@ -75,8 +78,9 @@ __device__ __forceinline__ void fp4_finite(float (&v)[kVec], float& top) {
 }
 
 // This lane's part of a block whose maximum is `top` (finite): returns the block's scale byte, puts the codes, eight a word, into `code`
-// and leaves the quotients x / step in `v`.  inv_unit, step_unit: 2^-exp and 2^exp of a tensor with blocks of 16.
-template <int BLOCK, int kVec>
+// and leaves the quotients x / step in `v`.  inv_unit, step_unit: 2^-exp and 2^exp of a tensor with blocks of 16.  SHORT: no element has
+// more than 16 significant bits.
+template <int BLOCK, int kVec, bool SHORT>
 __device__ __forceinline__ uint32_t fp4_encode(float (&v)[kVec], float top, float inv_unit, float step_unit, uint32_t (&code)[kVec / 8]) {
   uint32_t byte;
   if (BLOCK == 32) {
@@ -88,17 +92,17 @@ __device__ __forceinline__ uint32_t fp4_encode(float (&v)[kVec], float top, floa
     const float t = fminf(top * inv_unit, 3e38f), sixth = 1.f / 6.f, t6 = t * sixth;
     byte = e4m3_nearest(fmaf(fmaf(t6, 6.f, -t), -sixth, t6));
     const float s = e4m3_value(byte) * step_unit;
-    const float r = s > 0.f ? reciprocal(s) : 0.f;
+    const float r = s > 0.f ? __uint_as_float(__float_as_uint(reciprocal(s)) + (SHORT ? 4u : 0u)) : 0.f;
     if (top > 8.f * s) {
       // the largest scale was too small, or the smallest too large: beyond 8 steps all is clipped
 #pragma unroll
       for (int k = 0; k < kVec; ++k) v[k] = fminf(fmaxf(v[k], -8.f * s), 8.f * s);
     }
-    // (in this form a zero keeps its sign)
+    // (in both forms a zero keeps its sign)
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {
       const float q = v[k] * r;
-      v[k] = fmaf(fmaf(q, s, -v[k]), -r, q);
+      v[k] = SHORT ? __uint_as_float(__float_as_uint(q) & 0xfffffff0u) : fmaf(fmaf(q, s, -v[k]), -r, q);
     }
   }
 #pragma unroll

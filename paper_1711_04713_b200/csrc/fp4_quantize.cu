@@ -101,6 +101,15 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
+// max(a, |b|) of two pairs of 16-bit numbers, a >= 0; a NaN stays one.
+template <bool HALF>
+__device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (HALF) asm("{\n.reg .b32 t;\nabs.f16x2 t, %2;\nmax.NaN.f16x2 %0, %1, t;\n}\n" : "=r"(r) : "r"(a), "r"(b));
+  else asm("{\n.reg .b32 t;\nabs.bf16x2 t, %2;\nmax.NaN.bf16x2 %0, %1, t;\n}\n" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 // Quantizes one chunk; every lane of the warp comes along (n = 0: nothing to quantize, but codes and scales of the padding).
 template <int SRC, int BLOCK>
 __device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, uint32_t row, int col, int n, uint32_t (&w)[8],
@@ -155,7 +164,7 @@ __device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, 
 #pragma unroll
     for (int o = 1; o < BLOCK / kVec; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
   } else {
-    // magnitudes as 16-bit numbers, two at a time; relu: what has a sign is negative as a 16-bit number too
+    // two at a time; magnitudes are in order as 16-bit numbers, NaN above them all; relu: what has a sign is negative as a 16-bit number too
     uint32_t m = 0u;
     if (n < kVec) {
 #pragma unroll
@@ -164,7 +173,7 @@ __device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, 
 #pragma unroll
     for (int k = 0; k < kVec / 2; ++k) {
       if (p.relu) w[k] = __vmaxs2(w[k], 0u);
-      m = __vmaxu2(m, w[k] & 0x7fff7fffu);
+      m = max_abs2<SRC == kF16>(m, w[k]);
     }
     m = max(m & 0xffffu, m >> 16);
 #pragma unroll
@@ -184,7 +193,7 @@ __device__ __forceinline__ void quantize_chunk(const QuantParams& p, bool real, 
   }
   if (SRC != kPlanes) fp4_finite<BLOCK, kVec>(v, top);      // (a NaN fails its comparison)
   uint32_t code[kVec / 8];
-  const uint32_t byte = fp4_encode<BLOCK, kVec>(v, top, p.inv_unit, p.step_unit, code);
+  const uint32_t byte = fp4_encode<BLOCK, kVec, SRC != kF32>(v, top, p.inv_unit, p.step_unit, code);
   if (p.stats != nullptr) {
 #pragma unroll
     for (int k = 0; k < kVec; ++k) {

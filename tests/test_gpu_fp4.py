@@ -147,6 +147,65 @@ def test_quantize_large_and_every_float16():
         assert np.array_equal(got_byte, byte) and np.array_equal(got, code)
 
 
+@pytest.mark.parametrize("source", ["f32", "f16", "bf16", "fixed"])
+def test_quantize_next_to_every_border(source):
+    """For each step of E4M3: the numbers between two codes, and those next to them in the source's type, of both signs."""
+    frac = 15 - 12                                   # (16-bit fixed point holds 6 * 448)
+    rows = []
+    for s in ms.E4M3[1:]:
+        m = np.array([.25, .75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 0.01]) * s
+        if source == "fixed":
+            if s * 2 ** frac != np.floor(s * 2 ** frac):
+                continue                             # (the maximum, 6 steps, has to be a number of the source)
+            at = np.floor(m * 2 ** frac)
+            near = [(at + k) / 2 ** frac for k in (-1, 0, 1, 2)]
+        elif source == "bf16":
+            bits = (m.astype(np.float32).view(np.uint32) >> 16).astype(np.int64)
+            near = [((bits + k) << 16).astype(np.uint32).view(np.float32).astype(np.float64) for k in (-1, 0, 1, 2)]
+        else:
+            t = m.astype(np.float32 if source == "f32" else np.float16)
+            near = [np.nextafter(t, t.dtype.type(0)).astype(np.float64), t.astype(np.float64),
+                    np.nextafter(t, t.dtype.type(np.inf)).astype(np.float64)]
+        near = np.concatenate(near)
+        near = near[near <= 6 * s]
+        near = np.concatenate([near, -near])
+        for k in range(0, near.size, 15):
+            part = near[k:k + 15]
+            rows.append(np.concatenate([[6 * s], part, np.zeros(15 - part.size)]))
+    x = np.array(rows)
+    if source == "fixed":
+        whole = np.rint(x * 2 ** frac).astype(np.int64)
+        data, x = to_qtensor(whole, 16, frac, 16), whole / 2 ** frac       # (an integer holds no negative zero)
+    else:
+        data = dev(x.astype(np.float32)).to(DT[source])
+        assert np.array_equal(data.double().cpu().numpy(), x)
+    q = B.Fp4Tensor.empty(*x.shape, 16, 0)
+    st = B.new_stats()
+    B.adaption_fp4_quantize(data, *x.shape, q, False, st)
+    code, byte, counts = ms.quantize(x, 16, 0)
+    got, got_byte, _, _ = logical(q)
+    assert np.array_equal(got_byte, byte) and np.array_equal(got, code)
+    assert stats_tuple(st) == counts
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_quantize_special_values_of_16_bits(dtype, block):
+    tiny = 2.0 ** -24 if dtype == "f16" else 2.0 ** -133
+    vals = [np.nan, np.inf, -np.inf, 0.0, -0.0, tiny, -tiny, 3 * tiny, 60000.0, -60000.0, 448.0, 6.0, 7.0, -7.0, 5.0, 0.25]
+    x = np.array([vals + [0.0] * 16, [0.0] * 32, [np.nan] * 32, [np.inf] * 32, [tiny] * 32, vals[3:8] + [0.0] * 27, [-np.inf] + [1.0] * 31,
+                  [1.0] * 17 + [np.nan] + [-1.0] * 14])
+    data = torch.from_numpy(x).to(DT[dtype]).cuda()
+    x = data.double().cpu().numpy()
+    for exp in ((0,) if block == 32 else (0, -63, 63, -9)):
+        for relu in (False, True):
+            q = B.Fp4Tensor.empty(*x.shape, block, exp)
+            B.adaption_fp4_quantize(data, *x.shape, q, relu)
+            code, byte, _ = ms.quantize(x, block, exp, relu)
+            got, got_byte, _, _ = logical(q)
+            assert np.array_equal(got_byte, byte) and np.array_equal(got, code), (exp, relu)
+
+
 # --------------------------------------------------------------------------- values
 @pytest.mark.parametrize("block", [16, 32])
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
