@@ -314,11 +314,15 @@ ADAPTION_API int adaption_choose_frac_bits_from_acc(int64_t max_abs_acc, int32_t
  *             exponent for the whole tensor, -63 <= exp <= 63 (adaption_fp4_choose_exp).
  * Storage of a tensor of `outer` rows of `inner` elements:
  *   codes    rows of c_stride / 2 bytes, two elements a byte, the even one in bits 0-3; c_stride >= inner is
- *            a multiple of 32.  Behind the last element a row holds zeros.
+ *            a multiple of 32.  Behind the last element a row holds zeros.  The address is a multiple of 16.
  *   scales   adaption_fp4_scale_bytes(outer, inner, block) bytes: tiles of 128 rows x 4 blocks, 512 bytes each, the
  *            tiles of the same rows one after the other; inside a tile the byte of row r and block j is at
  *            (r % 32) * 16 + (r / 32) * 4 + j (the order in which the tensor cores take them).  The bytes of blocks
- *            behind a row's last one are 0; those of rows behind the last row are never read into a result. */
+ *            behind a row's last one are 0; those of rows behind the last row are never read into a result (nor written by
+ *            the quantizer).  The address is a multiple of 16.
+ * Sizes: rows of at most 2^24 elements (beyond: ADAPTION_ERR_K_TOO_LARGE from the products, ADAPTION_ERR_UNSUPPORTED from the others) and
+ * pitches of at most 2^25; at most 2^30 rows of either operand of a product.  A call of no rows does nothing.  What a call writes does
+ * not overlap what it reads; x and w may be the same tensor. */
 typedef struct adaption_fp4tensor {
   void* codes;
   void* scales;
@@ -372,8 +376,9 @@ ADAPTION_API int adaption_fp4_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_f
                                      void* stream);
 
 /* The same on real activations, which are quantized on the way as adaption_fp4_quantize does with w's block length
- * and the exponent x_exp.  The workspace takes their codes and scales (its contents need no initialisation); calls that may overlap
- * on the GPU need one each. */
+ * and the exponent x_exp, bit for bit what the two calls give.  The workspace, on a 16-byte boundary, takes their codes and scales (its
+ * contents need no initialisation); up to eight rows are quantized inside the product and leave it untouched.  Calls that may overlap
+ * on the GPU, replays of captured ones too, need one each. */
 ADAPTION_API size_t adaption_fp4_act_ip_workspace_bytes(int64_t B, int64_t K, int64_t O, int32_t block);
 ADAPTION_API int adaption_fp4_act_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_matrix x, int32_t x_exp,
                                          adaption_fp4tensor w, const float* d_bias, int32_t relu, adaption_matrix y,

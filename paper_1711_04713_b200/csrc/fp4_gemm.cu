@@ -667,8 +667,8 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   const uint32_t slot = (uint32_t)kgroups * 4u * (uint32_t)(1 + p.chunks_b);
   int stages = (int)((kSmemLimit - 1024 - (p.bulk ? 0 : received)) / p.stage_bytes);
   // more blocks than SMs: two share one, if that leaves each a ring of three stages
-  const int half = p.bulk ? 0 : (int)((kSmemLimit / 2 - 2048 - received) / p.stage_bytes);
-  if (tiles * per * p.S > num_sms() && half >= 3 && p.sf_col + 3u * slot <= 256u) {
+  const int half = (int)((kSmemLimit / 2 - 2048) / p.stage_bytes);
+  if (per * p.S == 1 && tiles > num_sms() && half >= 3 && p.sf_col + 3u * slot <= 256u) {
     stages = half;
     while (p.sf_col + (uint32_t)stages * slot > 256u) --stages;
   }
@@ -688,13 +688,10 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
     smem += received;
   }
   smem += 1024;
-  // CTAs that wait for one another take at least the share of an SM's shared memory that they take of its TMEM, so that what lies beside
-  // them never wants more columns than there are: two clusters (of two streams, say) that each hold columns which a CTA of the other one
-  // waits for would never end.
-  if (per * p.S > 1) {
-    const size_t least = p.tmem_cols > 256 ? kSmemLimit : (p.tmem_cols > 128 ? (size_t)112 * 1024 : (size_t)64 * 1024);
-    if (smem < least) smem = least;
-  }
+  // CTAs that wait for one another take all of an SM's shared memory, so that no block with TMEM columns lies beside them: two clusters
+  // (of two streams, say, one of them a layer's) that each hold columns which a CTA of the other one waits for would never end.  (Where
+  // the next call's blocks could come beside them, 4096 -> 4096 of one row took 3.6 us in a graph instead of 4.2; others the same.)
+  if (per * p.S > 1) smem = kSmemLimit;
   p.unit = pow2_float(g.x.exp + g.w.exp);
   p.bias = g.bias;
   p.relu = g.relu ? 1 : 0;

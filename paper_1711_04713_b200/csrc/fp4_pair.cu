@@ -437,7 +437,8 @@ int launch_fp4_pair(const Fp4Problem& g) {
   const int size = dtype_size(g.y.dtype);
   p.y = (uint8_t*)g.y.data;
   p.y_pitch = g.y.stride * size;
-  const bool rows = aligned16(g.y.data) && (p.y_pitch & 15) == 0 && (int64_t)p.O * size >= 16;
+  // (a store's coordinates are bytes, below 2^31)
+  const bool rows = aligned16(g.y.data) && (p.y_pitch & 15) == 0 && (int64_t)p.O * size >= 16 && (int64_t)p.O * size < (int64_t)1 << 31;
   p.cols16 = (int)(((int64_t)p.O * size & ~(int64_t)15) / size);
   const adaption_fp4tensor &ta = rows ? g.x : g.w, &tb = rows ? g.w : g.x;
   const int na = rows ? p.B : p.O, nb = rows ? p.O : p.B;

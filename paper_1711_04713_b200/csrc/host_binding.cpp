@@ -25,7 +25,7 @@ namespace {
   X(adaption_lp_conv_fwd_stochastic) X(adaption_lp_conv_pool_workspace_bytes) X(adaption_lp_conv_pool_fwd)           \
   X(adaption_lp_ip_workspace_bytes) X(adaption_lp_ip_fwd) X(adaption_lp_ip_fwd_stochastic)                           \
   X(adaption_lp_ip_fwd_static_ws) X(adaption_maxpool2x2)                                                             \
-  X(adaption_fp4_quantize) X(adaption_fp4_dequantize) X(adaption_fp4_ip_fwd) X(adaption_fp4_act_ip_fwd)
+  X(adaption_fp4_scale_bytes) X(adaption_fp4_quantize) X(adaption_fp4_dequantize) X(adaption_fp4_ip_fwd) X(adaption_fp4_act_ip_fwd)
 #define DECLARE(f) decltype(&::f) p_##f = nullptr;
 ADAPTION_FUNCTIONS(DECLARE)
 #undef DECLARE
@@ -599,12 +599,18 @@ int address(PyObject* t, long long device, void** out, size_t* bytes = nullptr) 
   if (bytes != nullptr) *bytes = (size_t)v.bytes;
   return 1;
 }
-int attr_address(PyObject* o, PyObject* name, long long device, void** out) {
+int attr_address(PyObject* o, PyObject* name, long long device, void** out, size_t* bytes = nullptr) {
   PyObject* t = PyObject_GetAttr(o, name);
   if (t == nullptr) return -1;
-  const int r = address(t, device, out);
+  const int r = address(t, device, out, bytes);
   Py_DECREF(t);
   return r;
+}
+// adaption_stats, or None
+int stats_address(PyObject* t, long long device, void** out) {
+  size_t bytes;
+  const int r = address(t, device, out, &bytes);
+  return r > 0 && *out != nullptr && bytes < sizeof(adaption_stats) ? 0 : r;
 }
 // Fp4Tensor of at least rows x cols
 int fp4tensor(PyObject* o, long long rows, long long cols, long long device, adaption_fp4tensor* f) {
@@ -613,12 +619,16 @@ int fp4tensor(PyObject* o, long long rows, long long cols, long long device, ada
       !attr_i64(o, s_block, &block) || !attr_i64(o, s_exp, &exp))
     return -1;
   // (the scale tiles follow from the row length, so a tensor is used at its own)
-  if (outer < rows || inner != cols) return 0;
+  if (outer < rows || inner != cols || cs < 0 || cs > (1ll << 40) || rows > (1ll << 40)) return 0;
   f->c_stride = cs;
   f->block = (int32_t)block;
   f->exp = exp < -1000 || exp > 1000 ? 1000 : (int32_t)exp;
-  const int a = attr_address(o, s_codes, device, &f->codes);
-  return a > 0 ? attr_address(o, s_scales, device, &f->scales) : a;
+  size_t codes = 0, scales = 0;
+  int r = attr_address(o, s_codes, device, &f->codes, &codes);
+  if (r > 0) r = attr_address(o, s_scales, device, &f->scales, &scales);
+  if (r <= 0) return r;
+  // (attributes can be given other tensors later)
+  return (unsigned __int128)rows * (unsigned long long)(cs / 2) <= codes && p_adaption_fp4_scale_bytes(rows, cols, f->block) <= scales;
 }
 // fp32 vector of at least n elements, or None
 int bias_vector(PyObject* t, long long n, long long device, void** out) {
@@ -661,7 +671,7 @@ PyObject* fp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     TAKE(matrix(a[0], outer, inner, dev, &x), where)
   }
   TAKE(fp4tensor(a[3], outer, inner, dev, &out), where)
-  TAKE(address(a[5], dev, &stats), where)
+  TAKE(stats_address(a[5], dev, &stats), where)
   CALL(p_adaption_fp4_quantize(x, fixed ? &q : nullptr, (size_t)outer, (size_t)inner, relu, out, (adaption_stats*)stats, st))
   return answer(rc, where);
 }
@@ -696,7 +706,7 @@ PyObject* fp4_ip_fwd(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   TAKE(fp4tensor(a[4], O, K, dev, &w), where)
   TAKE(bias_vector(a[5], O, dev, &bias), where)
   TAKE(matrix(a[7], B, O, dev, &y), where)
-  TAKE(address(a[8], dev, &stats), where)
+  TAKE(stats_address(a[8], dev, &stats), where)
   CALL(p_adaption_fp4_ip_fwd(B, K, O, x, w, (const float*)bias, relu, y, (adaption_stats*)stats, st))
   return answer(rc, where);
 }
@@ -719,7 +729,7 @@ PyObject* fp4_act_ip_fwd(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   TAKE(fp4tensor(a[5], O, K, dev, &w), where)
   TAKE(bias_vector(a[6], O, dev, &bias), where)
   TAKE(matrix(a[8], B, O, dev, &y), where)
-  TAKE(address(a[9], dev, &stats), where)
+  TAKE(stats_address(a[9], dev, &stats), where)
   TAKE(address(a[10], dev, &ws, &wsb), where)
   CALL(p_adaption_fp4_act_ip_fwd(B, K, O, x, (int32_t)x_exp, w, (const float*)bias, relu, y, (adaption_stats*)stats, ws, wsb, st))
   return answer(rc, where);

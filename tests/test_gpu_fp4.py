@@ -323,8 +323,8 @@ def test_every_number_of_shares(kernel, sizes):
 
 @pytest.mark.parametrize("block", [16, 32])
 def test_inner_product_of_more_tiles_than_the_gpu_has_pairs(block):
-    """85 tiles of 256 x 256: some pairs of CTAs work on a second one, in the other accumulator; every type, rows of outputs on
-    32-byte and 16-byte boundaries and off them."""
+    """85 tiles of 256 x 256: some pairs of CTAs work on a second one; every type, rows of outputs on 32-byte and 16-byte
+    boundaries and off them."""
     Bn = 1100
     for K, O, pad, dtype in ((300, 4112, 0, "f32"), (1300, 4112, 0, "bf16"), (64, 4104, 0, "f16"), (2900, 4101, 0, "f32"), (520, 4112, 1, "bf16"),
                              (200, 4110, 2, "f16"), (600, 4100, 4, "bf16")):
@@ -493,6 +493,92 @@ def test_repeated_and_concurrent_calls_give_the_same_bits():
     assert all(torch.equal(outs[0], y) for y in outs[1:])
 
 
+@pytest.mark.parametrize("kernel", ["cluster", "pairs", "persistent"])
+def test_a_tensor_times_itself(kernel):
+    choose(kernel)
+    rng = np.random.default_rng(8)
+    for rows, K in ((5, 96), (300, 1000)):
+        x, xv = operand(rng, rows, K, 16)
+        y, st = torch.empty(rows, rows, device="cuda"), B.new_stats()
+        B.adaption_fp4_ip_fwd(rows, K, rows, x, x, None, False, y, st)
+        check_product(y, xv, xv, None, False, 16, "f32")
+
+
+def test_products_of_two_streams_with_layers_beside_them():
+    """Products in clusters, and the layers' clusters, all of which hold TMEM while they wait for one another."""
+    rng = np.random.default_rng(18)
+    x, xv = operand(rng, 40, 4096, 16)
+    w, wv = operand(rng, 640, 4096, 16)
+    B_, K, O = 16, 1024, 512
+    xq = to_qtensor(rng.integers(-2000, 2000, (B_, K)), 16, 8, K)
+    wq = to_qtensor(rng.integers(-2000, 2000, (O, K)), 16, 8, K)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs, layers, st = [], [], B.new_stats()
+    work = [torch.empty(B_ * O * 8, dtype=torch.uint8, device="cuda") for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(30):
+        with torch.cuda.stream(streams[i % 3]):
+            if i % 2:
+                outs.append(torch.empty(40, 640, device="cuda"))
+                B.adaption_fp4_ip_fwd(40, 4096, 640, x, w, None, False, outs[-1], st)
+            else:
+                layers.append(B.QTensor.empty(B_, O, 16, 4))
+                B.adaption_lp_ip_fwd(B_, K, O, xq, wq, None, 0, False, B.MODE_REQUANT, B.ALGO_AUTO, layers[-1], st, work[i % 3])
+    torch.cuda.synchronize()
+    check_product(outs[0], xv, wv, None, False, 16, "f32")
+    assert all(torch.equal(outs[0], y) for y in outs[1:])
+    assert all(torch.equal(layers[0].lo, y.lo) and torch.equal(layers[0].hi, y.hi) for y in layers[1:])
+    assert B.read_stats(st).status == 0
+
+
+def test_quantizer_and_values_of_more_rows_than_one_launch_takes():
+    """Rows of 8 elements, more than 2^32 bytes of x and of y: the first rows, those around the second launch's first one, the last."""
+    inner, pitch, rows = 8, 36, (1 << 26) + 1000                    # (two pieces of a row of codes: 2^26 rows a launch)
+    rng = np.random.default_rng(6)
+    x = torch.zeros(rows, pitch, dtype=torch.bfloat16, device="cuda")
+    q = B.Fp4Tensor.empty(rows, inner, 16, -5)
+    q.codes.fill_(0xA5)
+    places = [0, (1 << 26) - 256, rows - rows % 128 - 256]
+    parts = [torch.from_numpy(rng.standard_normal((400, inner))).to(torch.bfloat16).cuda() for _ in places]
+    for at, part in zip(places, parts):
+        x[at:at + 400, :inner] = part[:rows - at]
+    B.adaption_fp4_quantize(x[:, :inner], rows, inner, q)
+    y = torch.empty(rows, pitch, dtype=torch.bfloat16, device="cuda")
+    B.adaption_fp4_dequantize(q, rows, inner, y[:, :inner])
+    for at in places:
+        n = min(400, rows - at)
+        ref = x[at:at + n, :inner].double().cpu().numpy()
+        code, byte, _ = ms.quantize(ref, 16, -5)
+        here = B.Fp4Tensor(n, inner, 32, 16, -5, q.codes[at * 16:(at + n) * 16], q.scales[at // 128 * 512:])
+        got, got_byte, pad, _ = logical(here)
+        assert np.array_equal(got, code) and np.array_equal(got_byte, byte) and not pad.any()
+        assert np.array_equal(y[at:at + n, :inner].double().cpu().numpy(), ms.values(code, byte, 16, -5))
+    assert int((q.codes.view(-1, 16)[1000:(1 << 26) - 256] != 0).sum()) == 0
+
+
+@pytest.mark.parametrize("kernel", ["cluster", "pairs", "persistent"])
+def test_outputs_beyond_32_bits_of_offset(kernel):
+    """y of more than 2^32 bytes: its first and last rows and channels."""
+    choose(kernel)
+    Bn, K, O = 1040, 64, (1 << 20) + 5
+    rng = np.random.default_rng(9)
+    x, xv = operand(rng, Bn, K, 32)
+    # weights of a few kinds of rows, so that the reference is small
+    code = rng.integers(0, 16, (256, K)).astype(np.uint8)
+    byte = rng.integers(120, 130, (256, K // 32)).astype(np.uint8)
+    kinds, wv = stored(code, byte, 32), ms.values(code, byte, 32)
+    times = -(-O // 256)
+    w = B.Fp4Tensor(O, K, K, 32, 0, kinds.codes.repeat(times)[:O * K // 2].contiguous(), kinds.scales.repeat(times))
+    y, st = torch.empty(Bn, O, device="cuda"), B.new_stats()
+    B.adaption_fp4_ip_fwd(Bn, K, O, x, w, None, False, y, st)
+    last = (O - 1) // 256 * 256
+    check_product(y[:, :256], xv, wv, None, False, 32, "f32")
+    check_product(y[:, last:], xv, wv[:O - last], None, False, 32, "f32")
+    for r in (0, 517, Bn - 1):
+        assert torch.equal(y[r], y[r, :256].repeat(times)[:O])
+    assert B.read_stats(st).status == 0
+
+
 def test_refusals_of_the_binding():
     q = B.Fp4Tensor.empty(4, 64, 16)
     x, y, st = torch.zeros(4, 64, device="cuda"), torch.zeros(4, 4, device="cuda"), B.new_stats()
@@ -518,6 +604,22 @@ def test_refusals_of_the_binding():
                  (4, 64, 4, q, B.Fp4Tensor.empty(4, 64, 32), None, False, y, st)):
         with pytest.raises(B.AdaptionError):
             B.adaption_fp4_ip_fwd(*args)
+    for name, short in (("codes", q.codes[:-1]), ("scales", q.scales[:-1]), ("codes", q.codes.cpu())):
+        other = B.Fp4Tensor.empty(4, 64, 16)
+        setattr(other, name, short)
+        with pytest.raises(B.AdaptionError):
+            B.adaption_fp4_quantize(x, 4, 64, other)
+        with pytest.raises(B.AdaptionError):
+            B.adaption_fp4_ip_fwd(4, 64, 4, q, other, None, False, y, st)
+    for stats in (st[:-1], torch.zeros(1, dtype=torch.uint8, device="cuda")):
+        with pytest.raises(B.AdaptionError):
+            B.adaption_fp4_ip_fwd(4, 64, 4, q, q, None, False, y, stats)
+        with pytest.raises(B.AdaptionError):
+            B.adaption_fp4_quantize(x, 4, 64, q, False, stats)
+    wide = B.Fp4Tensor(1, 64, (1 << 25) + 32, 16, 0, torch.zeros((1 << 24) + 16, dtype=torch.uint8, device="cuda"), q.scales)
+    with pytest.raises(B.AdaptionError) as e:
+        B.adaption_fp4_quantize(x[:1], 1, 64, wide)
+    assert e.value.status == B.ERR_UNSUPPORTED
     need = B.fp4_act_ip_workspace_bytes(4, 64, 4, 16)
     for ws in (None, torch.empty(need - 1, dtype=torch.uint8, device="cuda"), torch.empty(need, dtype=torch.uint8)):
         with pytest.raises(B.AdaptionError):
