@@ -377,7 +377,7 @@ ADAPTION_API int adaption_fp4_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_f
 
 /* The same on real activations, which are quantized on the way as adaption_fp4_quantize does with w's block length
  * and the exponent x_exp, bit for bit what the two calls give.  The workspace, on a 16-byte boundary, takes their codes and scales (its
- * contents need no initialisation); up to eight rows are quantized inside the product and leave it untouched.  Calls that may overlap
+ * contents need no initialisation); a few rows are quantized inside the product and leave it untouched.  Calls that may overlap
  * on the GPU, replays of captured ones too, need one each. */
 ADAPTION_API size_t adaption_fp4_act_ip_workspace_bytes(int64_t B, int64_t K, int64_t O, int32_t block);
 ADAPTION_API int adaption_fp4_act_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_matrix x, int32_t x_exp,
@@ -416,7 +416,7 @@ ADAPTION_API int adaption_probe_i8_peak(int32_t bn, int32_t pair, int32_t iters,
  *   "halo" 0|2     activations are copied once per filter tap and first layers are packed / one copy serves all taps
  *                  wherever it can, whatever the number of tiles                     (default 1: heuristic)
  *   "fused" 0|2    products on real activations quantize them in a launch of their own / in the product wherever one
- *                  CTA per tile or share runs it                                      (default 1: up to 8 rows)
+ *                  CTA per tile or share runs it                                      (default 1: a few rows)   
  *                  (products of 4-bit operands: "pair" 0|1 and "cluster" 2 choose the kernel, "cluster_size" its shares)
  *   "pdl" 0        layer kernels are launched without programmatic stream serialization (default 1)
  *   "timeout_us" t limit of every device-side wait in microseconds (default 0: two seconds)

@@ -23,7 +23,12 @@
 // thirds of the copied bytes per product.  The S CTAs (pairs) of a cluster take shares of the k-blocks; at the end each owns
 // a range of columns (runs of four), sends its partial sums of the others' columns to their shared memory, and adds what it
 // receives to its own.  Few columns are sent by the lanes (st.async, counted by an mbarrier at the owner); as that mbarrier counts
-// every 16 bytes apart, 5000 cycles for 256 columns, more than 32 go through shared memory and leave as one bulk copy per owner.
+// every 16 bytes apart, 5000 cycles for 256 columns, more than 32 go through shared memory and leave as a bulk copy per run.
+//
+// What bounds it: the weights' bytes from HBM where rows are few, 4.1 TB/s over a launch of 14 us (25088 -> 4096, one row: 58 MB; about 2 us
+// pass before the first k-block and 2 after the last); with more rows an SM's share of L2's reads, 64 bytes a cycle (the same on 256
+// rows: 128 CTAs copy 171 MB in 10.5 of 18.2 us); for small matrices the launch's chain of copies, MMAs, exchange and stores (4096 -> 4096,
+// one row: 4.2 us).
 #include <cuda.h>
 
 #include <cstring>
@@ -748,14 +753,14 @@ static int run_plan(const Fp4Problem& g, const FpPlan& plan) {
 
 int fp4_ip_impl(const Fp4Problem& g) { return run_plan(g, choose_plan(g)); }
 
-// Whether the product quantizes the activations itself.  K = 4096, 4096 channels, in a graph: one row 4.8 us against 5.4 with a launch of its
-// own (one by one 5.5 against 8), eight rows 5.2 against 5.5, sixteen 6.2 against 5.7; 25088 to 4096, one row 14.5 against 15.1, sixteen 34
-// against 16.
+// Whether the product quantizes the activations itself.  To 4096 channels, one call after the other, against a launch of its own: 4096
+// elements, one row 6.5 us against 9.3, eight 6.0 against 7.0, sixteen 6.9 against 6.9 (in a graph 6.8 against 5.6); 25088 elements, one row
+// 14.0 against 14.6, four 14.8 against 15.2, eight 16.1 against 15.4, sixteen 23 against 15.4; 12800, four 9.2 against 10.6, eight 9.8 against 8.9.
 static bool quantizes_itself(const Fp4Problem& g, const FpPlan& plan) {
   const int mode = knob(kFused);
   if (mode == 0 || plan.persistent || plan.pair) return false;
   if (mode == 2) return true;
-  return g.B <= 8;
+  return g.B <= (g.K <= 8192 ? 8 : 4);
 }
 
 int fp4_act_ip_impl(Fp4Problem& g, const adaption_fp4tensor& workspace) {

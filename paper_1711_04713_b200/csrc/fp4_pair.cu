@@ -17,6 +17,9 @@
 // three under way.  The 64 KB of a tile take 3500 cycles of the SM's share of L2's writes in any case; stored by the lanes
 // themselves they held up the issuing warp's barrier tests and MMAs for that long (1100 cycles a k-block), as stores issued
 // all at once they held up the copies.
+//
+// Measured: 8192 x 8192 x 8192, blocks of 16, to bf16 190 us (5.8 PFLOP/s) while the GPU is cool, 217 (5.1) when it runs at its power limit,
+// where clocks fall to 1.6 GHz; an estimate of MMAs alone is 150 at 1.92 GHz.  Blocks of 32: 181.
 #include <cuda.h>
 
 #include <cstring>

@@ -14,7 +14,7 @@
 //     for amax / 6 against the borders of E4M3.
 //     Sources of 16 bits need two: an x off a border is off by 2^-16 of it at least.  With r raised by four units in the last place
 //     the product lies above x / step by 2^-24 to 2^-20 of it; cut to 20 bits it is m on the border m, and stays on its side
-//     of every other.  (4096 x 25088 bf16 in blocks of 16: 46.1 us instead of 46.8.)
+//     of every other.  (4096 x 25088 bf16 in blocks of 16: 46.1 us instead of 46.8; with maxima two at a time 45.0.)
 #pragma once
 
 #include "fp4.cuh"
