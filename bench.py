@@ -757,6 +757,30 @@ def run_kernel(args):
         out = {"kernel": "ip", "shape": [a.B, a.Kin, a.O], "n_bits": a.n_bits, "ms": ms,
                "tops": 2.0 * macs / (ms / 1e3) / 1e12, "weight_gbs": bytes_w / (ms / 1e3) / 1e9,
                "frac_of_hbm": bytes_w / (ms / 1e3) / 1e9 / peaks["hbm_gbs"], "workspace_bytes": need}
+    elif a.kernel == "fp4_ip":
+        x = torch.randn(a.B, a.Kin, device="cuda", generator=g)
+        w = torch.randn(a.O, a.Kin, device="cuda", generator=g) * math.sqrt(2.0 / a.Kin)
+        ops = []
+        for t in (x, w):
+            exp = B.adaption_fp4_choose_exp(float(t.abs().max())) if a.block == 16 else 0
+            ops.append(B.Fp4Tensor.empty(t.shape[0], a.Kin, a.block, exp))
+            B.adaption_fp4_quantize(t, t.shape[0], a.Kin, ops[-1])
+        y = torch.empty(a.B, a.O, dtype=torch.bfloat16, device="cuda")
+        st = B.new_stats()
+        # copies of the weights that do not fit L2 together, in turn
+        ws = [ops[1]]
+        for _ in range(min(31, 256 * 1024 * 1024 // ops[1].codes.numel())):
+            ws.append(B.Fp4Tensor(a.O, a.Kin, ops[1].c_stride, a.block, ops[1].exp, ops[1].codes.clone(), ops[1].scales.clone()))
+        turn = iter(range(1 << 62))
+        ms = _time_ms(torch, lambda: B.adaption_fp4_ip_fwd(a.B, a.Kin, a.O, ops[0], ws[next(turn) % len(ws)], None, True, y, st),
+                      a.iters)
+        if B.read_stats(st).status != 0:
+            raise B.AdaptionError(B.read_stats(st).status, "fp4_ip")
+        flops = 2.0 * a.B * a.Kin * a.O
+        nbytes = (a.B + a.O) * a.Kin * (0.5 + 1.0 / a.block) + 2 * a.B * a.O
+        out = {"kernel": "fp4_ip", "shape": [a.B, a.Kin, a.O], "block": a.block, "weight_copies": len(ws), "ms": ms, "tflops": flops / (ms / 1e3) / 1e12,
+               "gbs": nbytes / (ms / 1e3) / 1e9, "frac_of_hbm": nbytes / (ms / 1e3) / 1e9 / peaks["hbm_gbs"],
+               "frac_of_4x_bf16": flops / (ms / 1e3) / 1e12 / (4.0 * peaks["bf16_burst"])}
     elif a.kernel == "peak":
         sms = torch.cuda.get_device_properties(0).multi_processor_count
         out = {"kernel": "peak", "sms": sms, "configs": []}
@@ -788,6 +812,14 @@ def run_kernel(args):
             hist = B.new_hist()
             ms = _time_ms(torch, lambda: B.adaption_bit_histogram(x, hist), a.iters)
             nbytes = 4 * n
+        elif a.kernel in ("fp4_quantize", "fp4_dequantize"):
+            q = B.Fp4Tensor.empty(outer, inner, a.block, -8 if a.block == 16 else 0)
+            B.adaption_fp4_quantize(x, outer, inner, q)
+            if a.kernel == "fp4_quantize":
+                ms = _time_ms(torch, lambda: B.adaption_fp4_quantize(x, outer, inner, q), a.iters)
+            else:
+                ms = _time_ms(torch, lambda: B.adaption_fp4_dequantize(q, outer, inner, x), a.iters)
+            nbytes = int((4.5 + 1.0 / a.block) * n)
         elif a.kernel == "squantize":
             q = B.QTensor.empty(outer, inner, a.n_bits, a.n_bits - 3)
             st = B.new_stats()
@@ -838,7 +870,8 @@ def main():
                     help="record per-layer CUDA events on every n-th timed step (roofline durations)")
     # one layer or one streaming kernel alone
     ap.add_argument("--kernel", default=None,
-                    choices=["conv", "ip", "peak", "streaming", "quantize", "squantize", "hist"])
+                    choices=["conv", "ip", "peak", "streaming", "quantize", "squantize", "hist", "fp4_quantize", "fp4_dequantize",
+                             "fp4_ip"])
     ap.add_argument("--N", type=int, default=8)
     ap.add_argument("--H", type=int, default=28)
     ap.add_argument("--C", type=int, default=512)
@@ -852,6 +885,7 @@ def main():
     ap.add_argument("--O", type=int, default=4096)
     ap.add_argument("--numel", type=int, default=1 << 28)
     ap.add_argument("--inner", type=int, default=256)
+    ap.add_argument("--block", type=int, default=16, choices=[16, 32], help="block length of a 4-bit tensor")
     ap.add_argument("--iters", type=int, default=20)
     ap.add_argument("--seed", type=int, default=0)
     ap.add_argument("--algo", type=int, default=0)

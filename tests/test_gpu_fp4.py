@@ -5,6 +5,8 @@ rounds (or cuts off) at most one unit in the last place, 2^-23, of a partial sum
 S = sum |x w| (+ |bias|); a row has at most one addition per scale block and per share of the reduction, two
 scalings that are exact, and one rounding to the output type, half a step.
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -577,6 +579,47 @@ def test_outputs_beyond_32_bits_of_offset(kernel):
     for r in (0, 517, Bn - 1):
         assert torch.equal(y[r], y[r, :256].repeat(times)[:O])
     assert B.read_stats(st).status == 0
+
+
+def test_calls_from_two_host_threads():
+    """Two host threads, each with its own stream, buffers and sizes, call at the same time and both get the definition's results."""
+    errors = []
+
+    def work(seed, Bn, K, O, block):
+        try:
+            torch.cuda.set_device(0)
+            rng = np.random.default_rng(seed)
+            with torch.cuda.stream(torch.cuda.Stream()):
+                w, wv = operand(rng, O, K, block, -2 if block == 16 else 0)
+                x = real_input(rng, Bn, K, "bf16")
+                ref = x.double().cpu().numpy()
+                exp = B.adaption_fp4_choose_exp(float(np.abs(ref).max())) if block == 16 else 0
+                code, byte, _ = ms.quantize(ref, block, exp)
+                ws = torch.empty(B.fp4_act_ip_workspace_bytes(Bn, K, O, block), dtype=torch.uint8, device="cuda")
+                for _ in range(20):
+                    y, st = torch.empty(Bn, O, device="cuda"), B.new_stats()
+                    B.adaption_fp4_act_ip_fwd(Bn, K, O, x, exp, w, None, False, y, st, ws)
+                check_product(y, ms.values(code, byte, block, exp), wv, None, False, block, "f32")
+        except Exception as exc:                              # noqa: BLE001 - reported to the main thread
+            errors.append(exc)
+
+    threads = [threading.Thread(target=work, args=a) for a in ((1, 3, 2000, 300, 16), (2, 200, 640, 520, 32))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+
+
+def test_leaves_that_want_gradients_are_read():
+    x = torch.randn(4, 64, device="cuda", requires_grad=True)
+    q, r = B.Fp4Tensor.empty(4, 64, 32), B.Fp4Tensor.empty(4, 64, 32)
+    B.adaption_fp4_quantize(x, 4, 64, q)
+    B.adaption_fp4_quantize(torch.nn.Parameter(x.detach().clone()), 4, 64, r)
+    code, byte, _ = ms.quantize(x.detach().double().cpu().numpy(), 32)
+    for t in (q, r):
+        got, got_byte, _, _ = logical(t)
+        assert np.array_equal(got, code) and np.array_equal(got_byte, byte)
 
 
 def test_refusals_of_the_binding():
