@@ -243,25 +243,29 @@ fp4_cluster_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const int o0 = (PAIR ? to * 2 + (int)half : to) * kRows, b0 = tb * p.BN;
   const int cols = min(p.BN, p.B - b0), col4 = (cols + 3) / 4;         // real columns, in runs of four
 
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < p.stages; ++s) {
-      mbar_init(smem_u32(&ctrl.full[s]), FUSED >= 0 ? 1 + cols : 1);
-      mbar_init(smem_u32(&ctrl.empty[s]), 1);
+  // (each of these steps takes 500 cycles: warps of their own, and a lane per barrier)
+  if (warp == 0) {
+    if (lane < p.stages) {
+      mbar_init(smem_u32(&ctrl.full[lane]), FUSED >= 0 ? 1 + cols : 1);
+      mbar_init(smem_u32(&ctrl.empty[lane]), 1);
+    } else if (lane == kMaxStages) {
+      mbar_init(smem_u32(&ctrl.done), 1);
+    } else if (lane == kMaxStages + 1) {
+      mbar_init(smem_u32(&ctrl.recv), 1);
+      ctrl.abort = 0;
     }
-    mbar_init(smem_u32(&ctrl.done), 1);
-    mbar_init(smem_u32(&ctrl.recv), 1);
-    ctrl.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 0 && lane < 4) prefetch_map(lane == 0 ? &map_a : (lane == 1 ? &map_b : (lane == 2 ? &map_sfa : &map_sfb)));
+  if (warp == 2 && lane < 4) prefetch_map(lane == 0 ? &map_a : (lane == 1 ? &map_b : (lane == 2 ? &map_sfa : &map_sfb)));
   if (warp == 1) {
     tmem_alloc<PAIR>(smem_u32(&ctrl.tmem_base), p.tmem_cols);
     tmem_relinquish<PAIR>();
   }
   tc_fence_before();
   __syncthreads();
-  // the barriers exist before another CTA signals them: a pair's at once, others when sums are sent
-  if (ctas > 1) cluster_arrive();
+  // the barriers exist before another CTA signals them: a pair's at once, others when sums are sent.  (The fence behind their
+  // initialisation is the release that this needs; another one waits 800 cycles.)
+  if (ctas > 1) cluster_arrive_relaxed();
   if (PAIR) cluster_wait();
   tc_fence_after();
   const uint32_t tmem = ctrl.tmem_base;
