@@ -587,6 +587,10 @@ int max_clusters(int dev, int sms, int ctas) {
   return n;
 }
 
+// Whether two single CTAs that wait for no other one fit on an SM, each with a ring of three stages or more: their ring's bytes.
+constexpr int64_t kHalfRing = (int64_t)(kSmemLimit / 2) - 2048;
+bool two_share_an_sm(int64_t stage_bytes) { return kHalfRing / stage_bytes >= 3; }
+
 struct FpPlan {
   bool pair = false, persistent = false;
   int S = 1, BN = 16;
@@ -594,10 +598,14 @@ struct FpPlan {
 };
 
 // Estimated cycles.  The form is that of the kernels: a k-block takes the time of its copies (an SM's share of L2's reads) or of its
-// MMAs, all operand bytes come from HBM at 4500 bytes a cycle at most, or 40 per SM at work; then the sums of the columns are exchanged and stored.  The constants are fitted to 290
-// runs, every number of shares of every form at 19 sizes from 1 to 4096 rows: 11 % off on average, and the choice at most 9 %
-// behind the best one (256 x 25088 -> 4096 18.5 us, the best 18.4; 512 x 4096 -> 4096 8.6, the best 8.0; 777 x 1411 -> 2049 6.8).
-FpPlan make_plan(const Fp4Problem& g, int only_pair) {
+// MMAs, all operand bytes come from HBM at 3950 bytes a cycle at most, or 100 per SM at work; then the sums of the columns are exchanged and
+// stored.  The constants are fitted to 395 runs, every number of shares of every form at 65 sizes from 1 to 4096 rows: 11 % off on
+// average, and the choice 1 % behind the best one, at most 13 % (256 x 25088 -> 4096 17.6 us, the best 17.6; 256 x 4096 -> 4096 6.5, the best 6.5;
+// 777 x 1411 -> 2049 6.1, the best 6.1; 4096 x 1024 -> 1024 6.4, the best 5.7).
+// quantizes: the activations are quantized in single CTAs' rings, where a k-block takes 300 cycles and 65 a row at least (25088 -> 4096, one
+// row: four shares 13.9 us, three 15.8; without it 12.3 and 12.5).
+FpPlan make_plan(const Fp4Problem& g, int only_pair, bool quantizes) {
+  constexpr double kStart = 3500;              // of a launch's or a wave's blocks, until their first k-block
   FpPlan best;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) dev = 64;
@@ -605,20 +613,22 @@ FpPlan make_plan(const Fp4Problem& g, int only_pair) {
   for (int form = 0; form < 3; ++form) {
     // single CTAs; pairs on up to 256 columns, and on 128 of more
     const bool pair = form > 0;
-    if ((only_pair >= 0 && pair != (only_pair != 0)) || (form == 2 && g.B <= kRows)) continue;
+    if ((only_pair >= 0 && pair != (only_pair != 0)) || (form == 2 && g.B <= kRows) || (quantizes && pair)) continue;
     const int tile_o = pair ? 2 * kRows : kRows, per = pair ? 2 : 1, most = form == 1 ? 2 * kRows : kRows;
     const int64_t bn = g.B < most ? (g.B + 15) / 16 * 16 : most;
     const int64_t tiles = ((g.O + tile_o - 1) / tile_o) * ((g.B + bn - 1) / bn);
-    const double bytes = (double)kABytes + (double)bn / per * kBlockBytes + (double)sf * (1 + (double)((bn + kRows - 1) / kRows));
-    const double mma = 4.0 * (bn > 160 ? (double)bn / 2 : 80.0) + 20.0, block = bytes / 60 > mma ? bytes / 60 : mma;
+    const int64_t stage = kABytes + bn / per * kBlockBytes + sf * (1 + (bn + kRows - 1) / kRows);
+    const double mma = quantizes ? 300.0 + 65.0 * (double)(g.B < bn ? g.B : bn) : 4.0 * (bn > 170 ? (double)bn / 2 : 85.0);
+    const double block = (double)stage / 75 > mma ? (double)stage / 75 : mma;
     const double operands = (double)g.K * ((double)g.O + (double)g.B) * (0.5 + 1.0 / g.w.block);
     for (int S = 1; S * per <= 8 && S <= kb; ++S) {
       const int64_t at_once = max_clusters(dev, sms, S * per);
-      const double waves = (double)((tiles + at_once - 1) / at_once);
-      const double exchange = (double)bn * (S > 1 ? 3.0 + (65.0 * (S - 1) + 3.0) / S : 24.0) + (pair ? 450.0 : 0.0);
-      const double ctas = (double)(tiles < at_once ? tiles : at_once) * S * per, all = operands / (ctas * 40.0 < 4500.0 ? ctas * 40.0 : 4500.0);
-      const double main_loop = waves * (double)((kb + S - 1) / S) * block;
-      const double cycles = (main_loop > all ? main_loop : all) + waves * (exchange + 4000.0) - 4000.0;      // (a wave's start)
+      const bool two = !pair && S == 1 && tiles > at_once && two_share_an_sm(stage);
+      const double waves = two ? (double)((tiles + 2 * at_once - 1) / (2 * at_once)) : (double)((tiles + at_once - 1) / at_once);
+      const double exchange = (double)bn * (S > 1 ? 0.5 + 100.0 * (S - 1) / S : (two ? 42.0 : 14.0)) + (pair ? 1950.0 : 0.0);
+      const double ctas = (double)(tiles < at_once ? tiles : at_once) * S * per, all = operands / (ctas * 100.0 < 3950.0 ? ctas * 100.0 : 3950.0);
+      const double main_loop = waves * (two ? 2.0 : 1.0) * (double)((kb + S - 1) / S) * block;
+      const double cycles = (main_loop > all ? main_loop : all) + waves * (exchange + kStart);
       if (cycles < best.cycles) {
         best.pair = pair;
         best.S = S;
@@ -627,11 +637,11 @@ FpPlan make_plan(const Fp4Problem& g, int only_pair) {
       }
     }
   }
-  if (only_pair < 0 && g.B > kRows) {
+  if (only_pair < 0 && g.B > kRows && !quantizes) {
     // the persistent kernel: tiles of 256 x 256 in turn, the stores of all but the last behind the next one's main loop
     const int64_t tiles = ((g.O + 255) / 256) * ((g.B + 255) / 256), pairs = sms / 2;
-    const double bytes = 2.0 * kABytes + 3.0 * sf, block = bytes / 64 > 512 ? bytes / 64 : 512;
-    const double cycles = (double)((tiles + pairs - 1) / pairs) * (kb * block + 4000.0) + 3500.0;
+    const double bytes = 2.0 * kABytes + 3.0 * sf, block = bytes / 65 > 512 ? bytes / 65 : 512;
+    const double cycles = (double)((tiles + pairs - 1) / pairs) * (kb * block + 3400.0) + 5000.0 + kStart;
     if (cycles < best.cycles) {
       best.persistent = true;
       best.cycles = cycles;
@@ -676,9 +686,8 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   const uint32_t slot = (uint32_t)kgroups * 4u * (uint32_t)(1 + p.chunks_b);
   int stages = (int)((kSmemLimit - 1024 - (p.bulk ? 0 : received)) / p.stage_bytes);
   // more blocks than SMs: two share one, if that leaves each a ring of three stages
-  const int half = (int)((kSmemLimit / 2 - 2048) / p.stage_bytes);
-  if (per * p.S == 1 && tiles > num_sms() && half >= 3 && p.sf_col + 3u * slot <= 256u) {
-    stages = half;
+  if (per * p.S == 1 && tiles > num_sms() && two_share_an_sm(p.stage_bytes) && p.sf_col + 3u * slot <= 256u) {
+    stages = (int)(kHalfRing / p.stage_bytes);
     while (p.sf_col + (uint32_t)stages * slot > 256u) --stages;
   }
   if (stages > kMaxStages) stages = kMaxStages;
@@ -735,7 +744,7 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
 
 }  // namespace
 
-static FpPlan choose_plan(const Fp4Problem& g) {
+static FpPlan choose_plan(const Fp4Problem& g, bool quantizes) {
   // (tests: one cluster per tile of single CTAs or of pairs, or the persistent kernel, wherever the call would run)
   const int pair = knob(kPair);
   FpPlan plan;
@@ -743,7 +752,7 @@ static FpPlan choose_plan(const Fp4Problem& g) {
     plan.persistent = true;
     return plan;
   }
-  plan = make_plan(g, pair);
+  plan = make_plan(g, pair, quantizes && pair != 1);
   const int shares = knob(kClusterSize) / (plan.pair ? 2 : 1), most = plan.pair ? 4 : 8;
   if (shares > 0) plan.S = shares < most ? shares : most;
   if (knob(kClusterBN) == 128 && plan.pair && g.B > kRows) plan.BN = kRows;
@@ -755,21 +764,18 @@ static int run_plan(const Fp4Problem& g, const FpPlan& plan) {
   return plan.persistent ? launch_fp4_pair(g) : launch_fp4_cluster(g, plan);
 }
 
-int fp4_ip_impl(const Fp4Problem& g) { return run_plan(g, choose_plan(g)); }
+int fp4_ip_impl(const Fp4Problem& g) { return run_plan(g, choose_plan(g, false)); }
 
 // Whether the product quantizes the activations itself.  To 4096 channels, one call after the other, against a launch of its own: 4096
 // elements, one row 6.5 us against 9.3, eight 6.0 against 7.0, sixteen 6.9 against 6.9 (in a graph 6.8 against 5.6); 25088 elements, one row
 // 14.0 against 14.6, four 14.8 against 15.2, eight 16.1 against 15.4, sixteen 23 against 15.4; 12800, four 9.2 against 10.6, eight 9.8 against 8.9.
-static bool quantizes_itself(const Fp4Problem& g, const FpPlan& plan) {
-  const int mode = knob(kFused);
-  if (mode == 0 || plan.persistent || plan.pair) return false;
-  if (mode == 2) return true;
-  return g.B <= (g.K <= 8192 ? 8 : 4);
-}
+static bool few_rows(const Fp4Problem& g) { return g.B <= (g.K <= 8192 ? 8 : 4); }
 
 int fp4_act_ip_impl(Fp4Problem& g, const adaption_fp4tensor& workspace) {
-  const FpPlan plan = choose_plan(g);
-  if (quantizes_itself(g, plan)) {
+  const int mode = knob(kFused);
+  const bool few = mode == 1 && few_rows(g);
+  const FpPlan plan = choose_plan(g, few);
+  if ((few || mode == 2) && !plan.persistent && !plan.pair) {
     g.x = workspace;
     g.x.codes = nullptr;
     return launch_fp4_cluster(g, plan);
