@@ -602,8 +602,8 @@ struct FpPlan {
 // stored.  The constants are fitted to 395 runs, every number of shares of every form at 65 sizes from 1 to 4096 rows: 11 % off on
 // average, and the choice 1 % behind the best one, at most 13 % (256 x 25088 -> 4096 17.6 us, the best 17.6; 256 x 4096 -> 4096 6.5, the best 6.5;
 // 777 x 1411 -> 2049 6.1, the best 6.1; 4096 x 1024 -> 1024 6.4, the best 5.7).
-// quantizes: the activations are quantized in single CTAs' rings, where a k-block takes 300 cycles and 65 a row at least (25088 -> 4096, one
-// row: four shares 13.9 us, three 15.8; without it 12.3 and 12.5).
+// quantizes: the activations may be quantized in single CTAs' rings, where a k-block takes 300 cycles and 65 a row at least (25088 -> 4096,
+// one row: four shares 13.9 us, three 15.8; of 4-bit operands 12.3 and 12.5).
 FpPlan make_plan(const Fp4Problem& g, int only_pair, bool quantizes) {
   constexpr double kStart = 3500;              // of a launch's or a wave's blocks, until their first k-block
   FpPlan best;
@@ -744,7 +744,14 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
 
 }  // namespace
 
-static FpPlan choose_plan(const Fp4Problem& g, bool quantizes) {
+// Whether the product quantizes the activations itself.  To 4096 channels, one call after the other, against a launch of its own: 4096
+// elements, one row 6.5 us against 9.3, eight 6.0 against 7.0, sixteen 6.9 against 6.9 (in a graph 6.8 against 5.6); 25088 elements, one row
+// 14.0 against 14.6, four 14.8 against 15.2, eight 16.1 against 15.4, sixteen 23 against 15.4; 12800, four 9.2 against 10.6, eight 9.8 against 8.9.
+static bool few_rows(const Fp4Problem& g) { return g.B <= (g.K <= 8192 ? 8 : 4); }
+
+// The plan goes by the sizes alone, not by where the activations are quantized: with few rows the product of 4-bit operands takes the
+// plan of the one that quantizes, so that both give the same bits.
+static FpPlan choose_plan(const Fp4Problem& g) {
   // (tests: one cluster per tile of single CTAs or of pairs, or the persistent kernel, wherever the call would run)
   const int pair = knob(kPair);
   FpPlan plan;
@@ -752,7 +759,7 @@ static FpPlan choose_plan(const Fp4Problem& g, bool quantizes) {
     plan.persistent = true;
     return plan;
   }
-  plan = make_plan(g, pair, quantizes && pair != 1);
+  plan = make_plan(g, pair, few_rows(g) && pair != 1);
   const int shares = knob(kClusterSize) / (plan.pair ? 2 : 1), most = plan.pair ? 4 : 8;
   if (shares > 0) plan.S = shares < most ? shares : most;
   if (knob(kClusterBN) == 128 && plan.pair && g.B > kRows) plan.BN = kRows;
@@ -764,18 +771,12 @@ static int run_plan(const Fp4Problem& g, const FpPlan& plan) {
   return plan.persistent ? launch_fp4_pair(g) : launch_fp4_cluster(g, plan);
 }
 
-int fp4_ip_impl(const Fp4Problem& g) { return run_plan(g, choose_plan(g, false)); }
-
-// Whether the product quantizes the activations itself.  To 4096 channels, one call after the other, against a launch of its own: 4096
-// elements, one row 6.5 us against 9.3, eight 6.0 against 7.0, sixteen 6.9 against 6.9 (in a graph 6.8 against 5.6); 25088 elements, one row
-// 14.0 against 14.6, four 14.8 against 15.2, eight 16.1 against 15.4, sixteen 23 against 15.4; 12800, four 9.2 against 10.6, eight 9.8 against 8.9.
-static bool few_rows(const Fp4Problem& g) { return g.B <= (g.K <= 8192 ? 8 : 4); }
+int fp4_ip_impl(const Fp4Problem& g) { return run_plan(g, choose_plan(g)); }
 
 int fp4_act_ip_impl(Fp4Problem& g, const adaption_fp4tensor& workspace) {
   const int mode = knob(kFused);
-  const bool few = mode == 1 && few_rows(g);
-  const FpPlan plan = choose_plan(g, few);
-  if ((few || mode == 2) && !plan.persistent && !plan.pair) {
+  const FpPlan plan = choose_plan(g);
+  if ((mode == 2 || (mode == 1 && few_rows(g))) && !plan.persistent && !plan.pair) {
     g.x = workspace;
     g.x.codes = nullptr;
     return launch_fp4_cluster(g, plan);

@@ -374,6 +374,28 @@ def test_product_of_real_activations(block, fused):
         assert s.status == 0 and s.zeros == 2 * int((y == 0).sum())
 
 
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("shape", [(1, 25088, 1000), (3, 4096, 4096), (4, 2048, 8000), (5, 300, 128), (8, 8192, 2048), (4, 12800, 2048), (9, 4096, 1000)])
+def test_product_of_few_real_rows_is_the_two_calls(shape, block):
+    """The reduction is shared the same way wherever the activations are quantized, so the sums have the same bits."""
+    Bn, K, O = shape
+    rng = np.random.default_rng(K + O)
+    x = real_input(rng, Bn, K, "bf16")
+    exp = -6 if block == 16 else 0
+    w, _ = operand(rng, O, K, block, 0, 12)          # (scales far enough apart that sums round)
+    q, st = B.Fp4Tensor.empty(Bn, K, block, exp), B.new_stats()
+    want = torch.empty(Bn, O, device="cuda")
+    B.adaption_fp4_quantize(x, Bn, K, q)
+    B.adaption_fp4_ip_fwd(Bn, K, O, q, w, None, False, want, st)
+    ws = torch.empty(B.fp4_act_ip_workspace_bytes(Bn, K, O, block), dtype=torch.uint8, device="cuda")
+    for fused in (0, 1, 2):
+        B.adaption_debug_set("fused", fused)
+        y = torch.empty_like(want)
+        B.adaption_fp4_act_ip_fwd(Bn, K, O, x, exp, w, None, False, y, st, ws)
+        assert torch.equal(y, want), fused
+    assert B.read_stats(st).status == 0
+
+
 @pytest.mark.parametrize("kernel", ["cluster", "pairs", "persistent"])
 def test_infinite_and_nan_results_stay_in_their_places(kernel):
     """A NaN scale of one row or one channel reaches that row or channel alone; ReLU keeps NaN; fp16 results beyond its range are infinite."""
