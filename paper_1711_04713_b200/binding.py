@@ -501,7 +501,9 @@ def adaption_choose_frac_bits_from_acc(max_abs_acc: int, acc_frac_bits: int, n_b
 # (any pitch of at least a row); tensors lie on the current device.
 def fp4_scale_bytes(outer: int, inner: int, block: int) -> int:
     """adaption_fp4_scale_bytes: bytes of the scale plane."""
-    return -(-outer // 128) * -(--(-inner // block) // 4) * 512 if outer > 0 and inner > 0 else 0
+    if outer <= 0 or inner <= 0 or block not in (16, 32):
+        return 0
+    return -(-outer // 128) * -(-inner // (4 * block)) * 512
 
 
 def adaption_fp4_choose_exp(max_abs: float) -> int:

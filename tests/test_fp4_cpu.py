@@ -102,6 +102,10 @@ def test_layouts_and_helpers(lib):
         assert lib.adaption_fp4_scale_bytes(rows, inner, block) == B.fp4_scale_bytes(rows, inner, block) == want
     for bad in ((0, 5, 16), (5, 0, 16), (5, 5, 8), (-1, 5, 32)):
         assert lib.adaption_fp4_scale_bytes(*bad) == 0
+    for bad in ((0, 5, 16), (5, 0, 16), (5, 5, 8), (5, 5, 0), (5, 5, -16), (-1, 5, 32)):
+        assert B.fp4_scale_bytes(*bad) == 0
+        with pytest.raises(B.AdaptionError):
+            B.Fp4Tensor.empty(max(bad[0], 1), max(bad[1], 1), bad[2] if bad[2] not in (16, 32) else 24, device="cpu")
     assert B.adaption_fp4_choose_exp(0.0) == -63
     assert B.adaption_fp4_choose_exp(2688.0) == 0 and B.adaption_fp4_choose_exp(np.nextafter(np.float32(2688), np.float32(1e9))) == 1
     assert B.adaption_fp4_choose_exp(2688.0 * 2.0 ** -9) == -9
