@@ -664,8 +664,9 @@ PyObject* fp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     long long rows, cols;
     if (!attr_i64(a[0], s_outer, &rows) || !attr_i64(a[0], s_inner, &cols)) return nullptr;
     if (rows < outer || cols < inner) return refuse(where);
-    void* low;
-    TAKE(attr_address(a[0], s_lo, dev, &low), where)
+    void* plane;
+    TAKE(attr_address(a[0], s_lo, dev, &plane), where)
+    TAKE(attr_address(a[0], s_hi, dev, &plane), where)
     if (!qtensor(a[0], &q)) return nullptr;
   } else {
     TAKE(matrix(a[0], outer, inner, dev, &x), where)

@@ -662,6 +662,11 @@ def test_refusals_of_the_binding():
         B.adaption_fp4_quantize(x[:, :32], 4, 32, q)                                             # a tensor of another row length
     with pytest.raises(B.AdaptionError):
         B.adaption_fp4_quantize(torch.zeros(5, 64, device="cuda"), 5, 64, q)                     # more rows than it has
+    for plane in ("lo", "hi"):
+        fixed = B.QTensor.empty(4, 64, 16, 8)
+        setattr(fixed, plane, getattr(fixed, plane).cpu())
+        with pytest.raises(B.AdaptionError):
+            B.adaption_fp4_quantize(fixed, 4, 64, q)
     for bias in (torch.zeros(4, device="cuda", dtype=torch.float64), torch.zeros(3, device="cuda"), torch.zeros(8, device="cuda")[::2], torch.zeros(4)):
         with pytest.raises(B.AdaptionError):
             B.adaption_fp4_ip_fwd(4, 64, 4, q, q, bias, False, y, st)
