@@ -416,7 +416,7 @@ ADAPTION_API int adaption_probe_i8_peak(int32_t bn, int32_t pair, int32_t iters,
  *   "halo" 0|2     activations are copied once per filter tap and first layers are packed / one copy serves all taps
  *                  wherever it can, whatever the number of tiles                     (default 1: heuristic)
  *   "fused" 0|2    products on real activations quantize them in a launch of their own / in the product wherever one
- *                  CTA per tile or share runs it                                      (default 1: a few rows)   
+ *                  CTA per tile or share runs it                                      (default 1: a few rows)
  *                  (products of 4-bit operands: "pair" 0|1 and "cluster" 2 choose the kernel, "cluster_size" its shares)
  *   "pdl" 0        layer kernels are launched without programmatic stream serialization (default 1)
  *   "timeout_us" t limit of every device-side wait in microseconds (default 0: two seconds)
