@@ -521,8 +521,15 @@ struct View {
   int dtype;                           // ADAPTION_F32, _F16 or _BF16, or 3
   int ndim;                            // shape and strides of at most two dimensions
   long long shape[2], stride[2];
-  long long bytes;
+  long long bytes, item;               // of all elements, of one
+  bool contiguous;
 };
+// Whether elements lie one after the other; called for every dimension, the last one first, with n = 1 at the start.
+bool dense(long long size, long long stride, long long* n) {
+  const bool ok = size == 1 || stride == *n;
+  *n *= size;
+  return ok;
+}
 
 bool view_by_attributes(PyObject* t, View* v) {
   PyObject* d = PyObject_CallMethodNoArgs(t, s_get_device);
@@ -540,16 +547,27 @@ bool view_by_attributes(PyObject* t, View* v) {
   bool ok = stride != nullptr && PyTuple_Check(shape) && PyTuple_Check(stride);
   if (ok) {
     v->ndim = (int)PyTuple_GET_SIZE(shape);
-    for (int k = 0; ok && k < v->ndim && k < 2; ++k)
-      ok = i64(PyTuple_GET_ITEM(shape, k), &v->shape[k]) && i64(PyTuple_GET_ITEM(stride, k), &v->stride[k]);
+    v->contiguous = true;
+    long long n = 1;
+    for (int k = v->ndim - 1; ok && k >= 0; --k) {
+      long long size, step;
+      ok = i64(PyTuple_GET_ITEM(shape, k), &size) && i64(PyTuple_GET_ITEM(stride, k), &step);
+      if (!ok) break;
+      if (k < 2) {
+        v->shape[k] = size;
+        v->stride[k] = step;
+      }
+      v->contiguous = dense(size, step, &n) && v->contiguous;
+    }
+    v->contiguous = v->contiguous || n == 0;
   } else if (!PyErr_Occurred()) {
     PyErr_SetString(PyExc_TypeError, "a tensor is expected");
   }
   Py_XDECREF(shape);
   Py_XDECREF(stride);
-  long long n = 0, item = 0;
-  if (!ok || !numel(t, &n) || !attr_i64(t, s_itemsize, &item)) return false;
-  v->bytes = n * item;
+  long long n = 0;
+  if (!ok || !numel(t, &n) || !attr_i64(t, s_itemsize, &v->item)) return false;
+  v->bytes = n * v->item;
   return tensor_ptr(t, &v->data);
 }
 bool view_of(PyObject* t, View* v) {
@@ -563,15 +581,19 @@ bool view_of(PyObject* t, View* v) {
   const int type = d.dtype.lanes != 1 ? 0 : d.dtype.code * 256 + d.dtype.bits;
   v->dtype = type == 2 * 256 + 32 ? ADAPTION_F32 : type == 2 * 256 + 16 ? ADAPTION_F16 : type == 4 * 256 + 16 ? ADAPTION_BF16 : 3;
   v->ndim = d.ndim;
+  v->contiguous = true;
   long long n = 1;
   for (int k = d.ndim - 1; k >= 0; --k) {
+    const long long step = d.strides != nullptr ? d.strides[k] : n;
     if (k < 2) {
       v->shape[k] = d.shape[k];
-      v->stride[k] = d.strides != nullptr ? d.strides[k] : n;
+      v->stride[k] = step;
     }
-    n *= d.shape[k];
+    v->contiguous = dense(d.shape[k], step, &n) && v->contiguous;
   }
-  v->bytes = n * (d.dtype.bits / 8);
+  v->contiguous = v->contiguous || n == 0;
+  v->item = (long long)d.dtype.bits * d.dtype.lanes / 8;
+  v->bytes = n * v->item;
   return true;
 }
 // 2-D tensor of rows x cols -> descriptor: 1, 0 (refused) or -1 (exception)
@@ -605,6 +627,35 @@ int attr_address(PyObject* o, PyObject* name, long long device, void** out, size
   const int r = address(t, device, out, bytes);
   Py_DECREF(t);
   return r;
+}
+// A byte plane of a fixed-point tensor (null for None): on the device and, where `need` bytes of it are read, holding them one after
+// the other.
+int plane_address(PyObject* o, PyObject* name, long long device, unsigned __int128 need, void** out) {
+  *out = nullptr;
+  PyObject* t = PyObject_GetAttr(o, name);
+  if (t == nullptr) return -1;
+  View v;
+  const int r = t == Py_None ? 0 : (view_of(t, &v) ? 1 : -1);
+  Py_DECREF(t);
+  if (r <= 0) return r < 0 ? -1 : 1;
+  if (v.device != device || (need > 0 && (v.item != 1 || !v.contiguous || (unsigned __int128)v.bytes < need))) return 0;
+  *out = v.data;
+  return 1;
+}
+// QTensor of at least rows x cols as a source
+int fixed_source(PyObject* o, long long rows, long long cols, long long device, adaption_qtensor* q) {
+  long long outer, inner, n, f, cs;
+  if (!attr_i64(o, s_outer, &outer) || !attr_i64(o, s_inner, &inner) || !attr_i64(o, s_n_bits, &n) || !attr_i64(o, s_frac_bits, &f) ||
+      !attr_i64(o, s_c_stride, &cs))
+    return -1;
+  if (outer < rows || inner < cols || cs < cols || n < 1 || n > 16 || f < 0 || f > 15) return 0;
+  const unsigned __int128 need = (unsigned __int128)rows * (unsigned long long)cs;
+  q->q16 = nullptr;
+  q->fmt.n_bits = (int32_t)n;
+  q->fmt.frac_bits = (int32_t)f;
+  q->c_stride = cs;
+  const int r = plane_address(o, s_lo, device, need, &q->lo);
+  return r > 0 ? plane_address(o, s_hi, device, n > 8 ? need : 0, &q->hi) : r;
 }
 // adaption_stats, or None
 int stats_address(PyObject* t, long long device, void** out) {
@@ -661,13 +712,7 @@ PyObject* fp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (outer < 0 || inner < 0) return refuse(where);
   const bool fixed = !PyObject_TypeCheck(a[0], (PyTypeObject*)g_tensor) && PyObject_HasAttr(a[0], s_n_bits);
   if (fixed) {
-    long long rows, cols;
-    if (!attr_i64(a[0], s_outer, &rows) || !attr_i64(a[0], s_inner, &cols)) return nullptr;
-    if (rows < outer || cols < inner) return refuse(where);
-    void* plane;
-    TAKE(attr_address(a[0], s_lo, dev, &plane), where)
-    TAKE(attr_address(a[0], s_hi, dev, &plane), where)
-    if (!qtensor(a[0], &q)) return nullptr;
+    TAKE(fixed_source(a[0], outer, inner, dev, &q), where)
   } else {
     TAKE(matrix(a[0], outer, inner, dev, &x), where)
   }
@@ -747,7 +792,7 @@ bool views_agree(PyObject* t) {
     return false;
   }
   return a.data == b.data && a.device == b.device && a.dtype == b.dtype && a.ndim == b.ndim && a.bytes == b.bytes &&
-         memcmp(a.shape, b.shape, sizeof(a.shape)) == 0 && memcmp(a.stride, b.stride, sizeof(a.stride)) == 0;
+         a.item == b.item && a.contiguous == b.contiguous && memcmp(a.shape, b.shape, sizeof(a.shape)) == 0 && memcmp(a.stride, b.stride, sizeof(a.stride)) == 0;
 }
 
 // library path, AdaptionError, current device, stream of device, the types of ADAPTION_F32, _F16 and _BF16, the tensor class, its
