@@ -609,14 +609,14 @@ int matrix(PyObject* t, long long rows, long long cols, long long device, adapti
   m->stride = rows > 1 ? v.stride[0] : (v.stride[0] > cols ? v.stride[0] : cols);
   return 1;
 }
-// a tensor's address (null for None) if it lies on the device; `bytes`: its size
+// a tensor's address (null for None) if it lies on the device and holds its elements one after the other; `bytes`: its size
 int address(PyObject* t, long long device, void** out, size_t* bytes = nullptr) {
   *out = nullptr;
   if (bytes != nullptr) *bytes = 0;
   if (t == Py_None) return 1;
   View v;
   if (!view_of(t, &v)) return -1;
-  if (v.device != device) return 0;
+  if (v.device != device || !v.contiguous) return 0;
   *out = v.data;
   if (bytes != nullptr) *bytes = (size_t)v.bytes;
   return 1;

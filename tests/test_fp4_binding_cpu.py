@@ -77,3 +77,30 @@ def test_planes_of_a_fixed_point_tensor_have_to_hold_its_rows():
         assert quantize_status(fixed(**bad)) == B.ERR_INVALID_ARG, bad
     assert quantize_status(fixed(8, lo=plane(ROWS * 80 - 1))) == B.ERR_INVALID_ARG
     assert quantize_status(fixed(8, hi=plane(1))) == B.ERR_CUDA                                # (a plane that eight bits do not use)
+
+
+def test_buffers_have_to_hold_their_bytes_one_after_the_other():
+    x, y, st = torch.zeros(ROWS, INNER), torch.zeros(ROWS, 5), B.new_stats("cpu")
+    w, good = four_bit(5), four_bit()
+    need = B.fp4_act_ip_workspace_bytes(ROWS, INNER, 5, 16)
+
+    def views(n):
+        return plane(1).expand(n), plane(1).expand(2, n), plane(2 * n)[::2], plane(2 * n).view(n, 2)[:, 0], plane(n).view(2, n // 2).t()
+
+    def calls(q=good, stats=st, ws=plane(need)):
+        return [status(B.adaption_fp4_quantize, x, ROWS, INNER, q, False, stats), status(B.adaption_fp4_dequantize, q, ROWS, INNER, x),
+                status(B.adaption_fp4_ip_fwd, ROWS, INNER, 5, q, w, None, False, y, stats),
+                status(B.adaption_fp4_act_ip_fwd, ROWS, INNER, 5, x, 0, w, None, False, y, stats, ws),
+                status(B.adaption_fp4_act_ip_fwd, ROWS, INNER, ROWS, x, 0, q, None, False, torch.zeros(ROWS, ROWS), stats, plane(2 * need))]
+
+    assert calls() == [B.ERR_CUDA] * 5
+    assert calls(ws=plane(need).view(2, need // 2)) == [B.ERR_CUDA] * 5
+    for ws in views(need):
+        assert calls(ws=ws)[3] == B.ERR_INVALID_ARG
+    for name in ("codes", "scales"):
+        for t in views(getattr(good, name).numel()):
+            got = calls(q=four_bit(**{name: t}))
+            assert got[:3] + got[4:] == [B.ERR_INVALID_ARG] * 4, (name, t.shape, t.stride())
+    for stats in views(B.STATS_BYTES):
+        got = calls(stats=stats)
+        assert [got[0]] + got[2:] == [B.ERR_INVALID_ARG] * 4
