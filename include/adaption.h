@@ -321,7 +321,7 @@ ADAPTION_API int adaption_choose_frac_bits_from_acc(int64_t max_abs_acc, int32_t
  *            behind a row's last one are 0; those of rows behind the last row are never read into a result (nor written by
  *            the quantizer).  The address is a multiple of 16.
  * Sizes: rows of at most 2^24 elements (beyond: ADAPTION_ERR_K_TOO_LARGE from the products, ADAPTION_ERR_UNSUPPORTED from the others) and
- * pitches of at most 2^25; at most 2^30 rows of either operand of a product.  A call of no rows does nothing.  What a call writes does
+ * pitches of at most 2^25; at most 2^30 rows of either operand of a product.  The counters' address is a multiple of 8.  A call of no rows does nothing.  What a call writes does
  * not overlap what it reads; x and w may be the same tensor. */
 typedef struct adaption_fp4tensor {
   void* codes;

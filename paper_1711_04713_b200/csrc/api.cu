@@ -231,6 +231,7 @@ static int build_fp4_problem(int64_t B, int64_t K, int64_t O, const adaption_fp4
   int rc = check_fp4(w, K);
   if (rc != ADAPTION_OK) return rc;
   if (stats == nullptr) return ADAPTION_ERR_INVALID_ARG;
+  if (!aligned_stats(stats)) return ADAPTION_ERR_ALIGNMENT;
   rc = B > 0 ? check_matrix(y, O) : ADAPTION_OK;        // (no rows: nothing of x or y is looked at)
   if (rc != ADAPTION_OK) return rc;
   if (bias != nullptr && (reinterpret_cast<uintptr_t>(bias) & 3u) != 0) return ADAPTION_ERR_ALIGNMENT;

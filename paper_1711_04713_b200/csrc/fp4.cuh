@@ -24,6 +24,8 @@ __device__ __forceinline__ uint32_t fp4_scale_offset(uint32_t r, int j, int grou
 
 int check_fp4(const adaption_fp4tensor& t, int64_t inner);
 int check_matrix(const adaption_matrix& m, int64_t inner);
+// (64-bit counters, added to by atomics)
+inline bool aligned_stats(const adaption_stats* s) { return (reinterpret_cast<uintptr_t>(s) & 7u) == 0; }
 
 int fp4_quantize_impl(const adaption_matrix& x, const adaption_qtensor* q, size_t outer, size_t inner, int32_t relu,
                       const adaption_fp4tensor& out, adaption_stats* stats, cudaStream_t stream);

@@ -430,6 +430,7 @@ int fp4_quantize_impl(const adaption_matrix& x, const adaption_qtensor* q, size_
   if (rc != ADAPTION_OK) return rc;
   rc = q != nullptr ? check_qtensor_in(*q, (int64_t)inner) : check_matrix(x, (int64_t)inner);
   if (rc != ADAPTION_OK) return rc;
+  if (!aligned_stats(stats)) return ADAPTION_ERR_ALIGNMENT;
   QuantParams p{};
   p.inner = (int)inner;
   p.c_stride = (int)out.c_stride;

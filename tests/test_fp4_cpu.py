@@ -212,3 +212,12 @@ def test_tensors_off_the_current_device_are_refused(lib):
                  lambda: B.adaption_fp4_ip_fwd(4, 64, 4, q, q, None, False, torch.zeros(4, 4), st)):
         with pytest.raises((B.AdaptionError, RuntimeError, AssertionError)):
             call()
+
+
+@pytest.mark.parametrize("off", [1, 2, 4])
+def test_counters_off_their_alignment_are_refused(lib, off):
+    """The kernels add 64-bit counters atomically."""
+    f, m = _fp4(), _mat()
+    assert lib.adaption_fp4_quantize(m, None, 3, 60, 0, f, FAKE + off, None) == B.ERR_ALIGNMENT
+    assert lib.adaption_fp4_ip_fwd(3, 60, 60, f, f, None, 0, m, FAKE + off, None) == B.ERR_ALIGNMENT
+    assert lib.adaption_fp4_act_ip_fwd(3, 60, 60, m, 0, f, None, 0, m, FAKE + off, FAKE, 1 << 20, None) == B.ERR_ALIGNMENT
