@@ -368,7 +368,7 @@ ADAPTION_API int adaption_fp4_dequantize(adaption_fp4tensor x, size_t outer, siz
 
 /* Inner product of 4-bit operands: y[b,o] = act(sum_k x[b,k] * w[o,k] + bias[o]), x [B][K] and w [O][K] of the same
  * block length, bias fp32 [O] or NULL, act ReLU if relu != 0, y [B][O].  Products are exact, sums are held in 32-bit
- * floating point in an order fixed by the sizes (so that the same call gives the same bits), and the result is
+ * floating point in an order fixed by the sizes and the kind of device (so that the same call gives the same bits on one device), and the result is
  * rounded once to the type of y.  Rows of y are aligned to the element only.  d_stats (not NULL) counts outputs equal to 0
  * and takes the status. */
 ADAPTION_API int adaption_fp4_ip_fwd(int64_t B, int64_t K, int64_t O, adaption_fp4tensor x, adaption_fp4tensor w,

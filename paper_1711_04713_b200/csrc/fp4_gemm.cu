@@ -36,6 +36,7 @@
 #include "fp4_mma.cuh"
 #include "fp4_quant.cuh"
 #include "knobs.cuh"
+#include "remember.cuh"
 #include "tensor_maps.cuh"
 
 namespace adaption {
@@ -556,35 +557,34 @@ int launch_fused(const CUtensorMap* maps, const FpParams& p, int x_dtype, int gr
 }
 
 // Clusters of `ctas` blocks, one block per SM, that the current device runs at a time.  (A cluster stays inside one group of SMs, so
-// there are fewer than SMs / ctas: 74 of 2, 33 of 4, 22 of 6, 15 of 8 on 148 SMs.)  Asked once per device and size.
+// there are fewer than SMs / ctas: 74 of 2, 33 of 4, 22 of 6, 15 of 8 on 148 SMs.)  Asked once per device and size; a guess where the
+// device does not answer.
 int max_clusters(int dev, int sms, int ctas) {
   constexpr int kMaxDevices = 64, kMaxCtas = 8;
   static std::atomic<int> known[kMaxDevices][kMaxCtas + 1];
   if (ctas == 1) return sms;
-  if (dev < kMaxDevices) {
-    const int n = known[dev][ctas].load(std::memory_order_relaxed);
-    if (n > 0) return n;
-  }
-  int n = 0;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(threads_of(true, false));
-  cfg.dynamicSmemBytes = kSmemLimit;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = (unsigned)ctas;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const auto kernel = fp4_cluster_kernel<16, true, ADAPTION_BF16, -1>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit) != cudaSuccess ||
-      cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
-    (void)cudaGetLastError();
-    n = sms / (ctas > 4 ? ctas + 1 : ctas);
-    if (n < 1) n = 1;
-  }
-  if (dev < kMaxDevices) known[dev][ctas].store(n, std::memory_order_relaxed);
-  return n;
+  std::atomic<int> nowhere{0};
+  const int guess = sms / (ctas > 4 ? ctas + 1 : ctas);
+  return remembered(dev < kMaxDevices ? known[dev][ctas] : nowhere, guess > 1 ? guess : 1, [ctas]() {
+    int n = 0;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3(threads_of(true, false));
+    cfg.dynamicSmemBytes = kSmemLimit;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const auto kernel = fp4_cluster_kernel<16, true, ADAPTION_BF16, -1>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+      (void)cudaGetLastError();
+      return 0;
+    }
+    return n;
+  });
 }
 
 // Whether two single CTAs that wait for no other one fit on an SM, each with a ring of three stages or more: their ring's bytes.
@@ -749,7 +749,7 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
 // 14.0 against 14.6, four 14.8 against 15.2, eight 16.1 against 15.4, sixteen 23 against 15.4; 12800, four 9.2 against 10.6, eight 9.8 against 8.9.
 static bool few_rows(const Fp4Problem& g) { return g.B <= (g.K <= 8192 ? 8 : 4); }
 
-// The plan goes by the sizes alone, not by where the activations are quantized: with few rows the product of 4-bit operands takes the
+// The plan goes by the sizes (and the device) alone, not by where the activations are quantized: with few rows the product of 4-bit operands takes the
 // plan of the one that quantizes, so that both give the same bits.
 static FpPlan choose_plan(const Fp4Problem& g) {
   // (tests: one cluster per tile of single CTAs or of pairs, or the persistent kernel, wherever the call would run)

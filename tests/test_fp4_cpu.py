@@ -1,5 +1,6 @@
 """Microscaled 4-bit operators without a GPU: the oracle's pins, host helpers, and refusals before any launch."""
 import ctypes
+import subprocess
 from fractions import Fraction
 
 import numpy as np
@@ -221,3 +222,27 @@ def test_counters_off_their_alignment_are_refused(lib, off):
     assert lib.adaption_fp4_quantize(m, None, 3, 60, 0, f, FAKE + off, None) == B.ERR_ALIGNMENT
     assert lib.adaption_fp4_ip_fwd(3, 60, 60, f, f, None, 0, m, FAKE + off, None) == B.ERR_ALIGNMENT
     assert lib.adaption_fp4_act_ip_fwd(3, 60, 60, m, 0, f, None, 0, m, FAKE + off, FAKE, 1 << 20, None) == B.ERR_ALIGNMENT
+
+
+def test_a_question_that_failed_is_asked_again(tmp_path):
+    """How the cost model keeps the number of clusters that a device runs at a time: its guess stands for one call only."""
+    source, program = tmp_path / "ask.cpp", tmp_path / "ask"
+    source.write_text("""
+#include "remember.cuh"
+#include <cstdio>
+int main() {
+  std::atomic<int> slot{0};
+  int asked = 0, answer = 0;
+  const auto ask = [&]() { ++asked; return answer; };
+  const auto get = [&]() { return adaption::remembered(slot, 9, ask); };
+  std::printf("%d", get());
+  answer = -3;
+  std::printf(" %d", get());
+  answer = 33;
+  std::printf(" %d", get());
+  answer = 0;
+  std::printf(" %d %d\\n", get(), asked);
+}
+""")
+    subprocess.check_call(["g++", "-std=c++17", "-I", build.CSRC, str(source), "-o", str(program)])
+    assert subprocess.check_output([str(program)]).split() == [b"9", b"9", b"33", b"33", b"3"]
