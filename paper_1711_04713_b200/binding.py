@@ -306,9 +306,6 @@ class Fp4Tensor:
         scales = torch.empty(fp4_scale_bytes(outer, inner, block), dtype=torch.uint8, device=device)
         return Fp4Tensor(outer, inner, cs, block, exp, codes, scales)
 
-    def c_struct(self) -> adaption_fp4tensor:
-        return adaption_fp4tensor(_ptr(self.codes), _ptr(self.scales), self.c_stride, self.block, self.exp)
-
 
 def new_stats(device="cuda") -> torch.Tensor:
     """Zeroed device-resident adaption_stats (as raw bytes)."""

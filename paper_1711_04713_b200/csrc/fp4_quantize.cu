@@ -388,13 +388,18 @@ __global__ void __launch_bounds__(kValueThreads) fp4_values_shifted_kernel(const
 
 unsigned blocks_of(uint32_t total, int per_block) { return (total + (uint32_t)per_block - 1) / (uint32_t)per_block; }
 
+template <int SRC, int BLOCK, bool ALIGNED>
+int launch_quantize(const QuantParams& p, cudaStream_t stream) {
+  const dim3 grid(blocks_of(p.total, kThreads * (ALIGNED ? kAhead : 1))), block(kThreads);
+  return cuda_status(launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, ALIGNED>, grid, block, stream, p), "fp4_quantize_kernel launch");
+}
+// (planes always lie on 16-byte boundaries)
 template <int SRC, int BLOCK>
 int launch_quantize(const QuantParams& p, bool aligned, cudaStream_t stream) {
-  aligned = aligned || SRC == kPlanes;
-  const dim3 grid(blocks_of(p.total, kThreads * (aligned ? kAhead : 1))), block(kThreads);
-  return cuda_status(aligned ? launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, true>, grid, block, stream, p)
-                             : launch_after_predecessor(fp4_quantize_kernel<SRC, BLOCK, false>, grid, block, stream, p),
-                     "fp4_quantize_kernel launch");
+  if constexpr (SRC != kPlanes) {
+    if (!aligned) return launch_quantize<SRC, BLOCK, false>(p, stream);
+  }
+  return launch_quantize<SRC, BLOCK, true>(p, stream);
 }
 template <int SRC>
 int launch_quantize(const QuantParams& p, int block, bool aligned, cudaStream_t stream) {
