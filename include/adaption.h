@@ -333,7 +333,8 @@ typedef struct adaption_fp4tensor {
 
 /* Real-valued matrices: rows of elements of one type, `stride` elements apart (at least a row's length).  The
  * address is aligned to the element; rows whose address and stride are multiples of 16 bytes are read and written
- * fastest. */
+ * fastest.  Other rows are read by the aligned 16-byte words that hold their elements: up to 15 bytes before a row and behind it
+ * are read too, never those of a 16-byte word that holds none of its elements, and have no effect.  Nothing but the elements is written. */
 enum { ADAPTION_F32 = 0, ADAPTION_F16 = 1, ADAPTION_BF16 = 2 };
 typedef struct adaption_matrix {
   void* data;
