@@ -347,7 +347,7 @@ typedef struct adaption_matrix {
 ADAPTION_API size_t adaption_fp4_scale_bytes(int64_t outer, int64_t inner, int32_t block);
 
 /* Host helper, the counterpart of the decimal point for blocks of 16: the smallest exponent in [-63, 63] with which
- * the scale of a block that holds max_abs fits E4M3 (max_abs <= 6 * 448 * 2^exp); -63 for 0.  max_abs must
+ * the scale of a block that holds max_abs fits E4M3 (max_abs <= 6 * 448 * 2^exp); -63 for 0, 63 where none fits.  max_abs must
  * not be negative or NaN. */
 ADAPTION_API int adaption_fp4_choose_exp(float max_abs, int32_t* h_exp);
 

@@ -25,10 +25,10 @@
 // receives to its own.  Few columns are sent by the lanes (st.async, counted by an mbarrier at the owner); as that mbarrier counts
 // every 16 bytes apart, 5000 cycles for 256 columns, more than 32 go through shared memory and leave as a bulk copy per run.
 //
-// What bounds it: the weights' bytes from HBM where rows are few, 4.1 TB/s over a launch of 14 us (25088 -> 4096, one row: 58 MB; about 2 us
-// pass before the first k-block and 2 after the last); with more rows an SM's share of L2's reads, 64 bytes a cycle (the same on 256
-// rows: 128 CTAs copy 171 MB in 10.5 of 18.2 us); for small matrices the launch's chain of copies, MMAs, exchange and stores (4096 -> 4096,
-// one row: 4.2 us).
+// What bounds it (replays of a graph over weights that do not fit L2 together): the weights' bytes from HBM where rows are few, 4.9 TB/s over a
+// launch of 11.8 us (25088 -> 4096, one row: 58 MB; about 2 us pass before the first k-block and 2 after the last; 15.1 us where the row is
+// quantized here); with more rows an SM's share of L2's reads, 64 bytes a cycle (the same on 256 rows: 128 CTAs copy 171 MB in 10.5 of
+// 17.9 us); for small matrices the launch's chain of copies, MMAs, exchange and stores (4096 -> 4096, one row: 4.8 us, 3.9 with the weights in L2).
 #include <cuda.h>
 
 #include <cstring>
@@ -600,10 +600,10 @@ struct FpPlan {
 // Estimated cycles.  The form is that of the kernels: a k-block takes the time of its copies (an SM's share of L2's reads) or of its
 // MMAs, all operand bytes come from HBM at 3950 bytes a cycle at most, or 100 per SM at work; then the sums of the columns are exchanged and
 // stored.  The constants are fitted to 395 runs, every number of shares of every form at 65 sizes from 1 to 4096 rows: 11 % off on
-// average, and the choice 1 % behind the best one, at most 13 % (256 x 25088 -> 4096 17.6 us, the best 17.6; 256 x 4096 -> 4096 6.5, the best 6.5;
-// 777 x 1411 -> 2049 6.1, the best 6.1; 4096 x 1024 -> 1024 6.4, the best 5.7).
+// average, and the choice 1 % behind the best one, at most 13 % (in graphs, three sets of operands in turn: 256 x 25088 -> 4096 17.6 us, the best
+// 17.6; 256 x 4096 -> 4096 6.5, the best 6.5; 777 x 1411 -> 2049 6.1, the best 6.1; 4096 x 1024 -> 1024 6.4, the best 5.7).
 // quantizes: the activations may be quantized in single CTAs' rings, where a k-block takes 300 cycles and 65 a row at least (25088 -> 4096,
-// one row: four shares 13.9 us, three 15.8; of 4-bit operands 12.3 and 12.5).
+// one row, the same way: four shares 13.9 us, three 15.8; of 4-bit operands 12.3 and 12.5).
 FpPlan make_plan(const Fp4Problem& g, int only_pair, bool quantizes) {
   constexpr double kStart = 3500;              // of a launch's or a wave's blocks, until their first k-block
   FpPlan best;
@@ -708,7 +708,7 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
   smem += 1024;
   // CTAs that wait for one another take all of an SM's shared memory, so that no block with TMEM columns lies beside them: two clusters
   // (of two streams, say, one of them a layer's) that each hold columns which a CTA of the other one waits for would never end.  (Where
-  // the next call's blocks could come beside them, 4096 -> 4096 of one row took 3.6 us in a graph instead of 4.2; others the same.)
+  // the next call's blocks could come beside them, 4096 -> 4096 of one row with two sets of weights in L2 took 3.6 us in a graph instead of 4.2; others the same.)
   if (per * p.S > 1) smem = kSmemLimit;
   p.unit = pow2_float(g.x.exp + g.w.exp);
   p.bias = g.bias;
@@ -747,6 +747,9 @@ int launch_fp4_cluster(const Fp4Problem& g, const FpPlan& plan) {
 // Whether the product quantizes the activations itself.  To 4096 channels, one call after the other, against a launch of its own: 4096
 // elements, one row 6.5 us against 9.3, eight 6.0 against 7.0, sixteen 6.9 against 6.9 (in a graph 6.8 against 5.6); 25088 elements, one row
 // 14.0 against 14.6, four 14.8 against 15.2, eight 16.1 against 15.4, sixteen 23 against 15.4; 12800, four 9.2 against 10.6, eight 9.8 against 8.9.
+// To more channels, where more tiles quantize the same rows, the rule is up to 13 % behind the better form (weights not in L2): eight
+// rows of 4096 to 11008 channels 12.1 against 10.7, to 28672 17.0 against 16.5, of 2048 to 57344 18.9 against 17.0; one of 4096 to 28672 14.2
+// against 15.6.
 static bool few_rows(const Fp4Problem& g) { return g.B <= (g.K <= 8192 ? 8 : 4); }
 
 // The plan goes by the sizes (and the device) alone, not by where the activations are quantized: with few rows the product of 4-bit operands takes the

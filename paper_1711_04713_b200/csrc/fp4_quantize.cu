@@ -3,8 +3,8 @@
 // Both are one pass over memory.  A lane takes a chunk of 32 bytes of a row's real values (8 or 16 elements); the lanes of a
 // block, at most four, find its maximum with shuffles, so that the values are read once and stay in registers.
 //
-// Bound by HBM: 200704 x 256 fp32 into blocks of 32 33.9 us (6.87 TB/s), its values 36.9 (6.3 TB/s; to bf16 6.5).  16-bit sources into
-// blocks of 16 by instructions as well: 4096 x 25088 bf16 45.0 us (5.85 TB/s, 11 instructions an element, issue slots 73 % busy).
+// Bound by HBM (in graphs; call after call 0.5 us more): 200704 x 256 fp32 into blocks of 32 34.0 us (6.85 TB/s), its values 36.9 (6.3 TB/s; to bf16
+// 6.5).  16-bit sources into blocks of 16 by instructions as well: 4096 x 25088 bf16 45.8 us (5.75 TB/s, 11 instructions an element, issue slots 73 % busy).
 #include "fp4_quant.cuh"
 
 namespace adaption {
